@@ -298,6 +298,89 @@ typedef enum {
 } moe_ffn_variant_id;
 moe_status moe_set_ffn_variant(moe_ctx *ctx, int32_t variant);
 
+/*
+ * The key/value cache and its attention: what stands beside the expert layer in a decoder block, for the same hybrid batches
+ * of decode rows and prompt rows.
+ *
+ * The cache is cut into pages of `page` tokens.  k_pages, v_pages [n_pages, kv_heads, page, dim] hold the context's dtype
+ * (MOE_KV_DTYPE) or FP8 E4M3 codes (MOE_KV_FP8: finite up to 448, no infinities, 0x7f and 0xff are NaN) with one E8M0 scale
+ * byte per token and head in k_scales, v_scales [n_pages, kv_heads, page]: a value is code * 2^(byte - 127), and the byte 255
+ * makes it NaN.  A batch is n_seqs sequences.  Sequence s brings the rows row_offsets[s] .. row_offsets[s+1] - 1 of the new tokens'
+ * tensors (row_offsets [n_seqs + 1] int32, from 0 to T without descending; empty sequences are legal); with them it holds
+ * kv_lens[s] tokens, of which they are the last: row i of n stands at position kv_lens[s] - n + i.  Token j lies in slot
+ * j % page of page page_table[s, j / page] (page_table [n_seqs, max_pages] int32).
+ * A token whose table entry is not in [0, n_pages), or lies beyond max_pages, is not there: nothing is written for it, nothing sees
+ * it, and it reads back as zeros.  Entries of pages that a sliding window has left behind are set to -1 that way.  (Where a position
+ * is negative, because kv_lens[s] is less than the sequence's rows, the row is not written, and sees nothing under a causal mask.)
+ * Descriptors live on the device and are read by every call, so a captured graph replays with what they then hold.
+ */
+typedef enum { MOE_KV_DTYPE = 0, MOE_KV_FP8 = 1 } moe_kv_format;
+
+typedef struct {
+    int32_t heads;     /* query heads, a multiple of kv_heads: head h reads key/value head h / (heads / kv_heads) */
+    int32_t kv_heads;
+    int32_t dim;       /* of a head: a multiple of 16, 16..256 */
+    int32_t page;      /* tokens of a page: a power of two, 8..256 */
+    int32_t dtype;     /* moe_dtype of queries, new keys and values, and outputs */
+    int32_t kv_format; /* moe_kv_format */
+} moe_kv_config;
+
+/* The pages of one layer (device pointers); the scales are read with MOE_KV_FP8 only. */
+typedef struct {
+    void *k_pages, *v_pages;
+    uint8_t *k_scales, *v_scales;
+    int64_t n_pages;   /* 1 or more */
+} moe_kv_pages;
+
+typedef struct {
+    const int32_t *row_offsets; /* [n_seqs + 1] */
+    const int32_t *kv_lens;     /* [n_seqs] */
+    const int32_t *page_table;  /* [n_seqs, max_pages] */
+    int64_t n_seqs, max_pages;
+} moe_kv_batch;
+
+typedef struct moe_kv_ctx moe_kv_ctx; /* opaque, host memory, owned by the library */
+
+/* Workspace of a context (partial results of the attention; the size depends on cfg alone), and the context, which keeps it
+ * like a moe_ctx does: calls on one context must not overlap in time.  The workspace needs no clearing; nothing is enqueued. */
+moe_status moe_kv_workspace_bytes(const moe_kv_config *cfg, size_t *out_bytes);
+moe_status moe_kv_create(const moe_kv_config *cfg, void *workspace, size_t workspace_bytes, moe_kv_ctx **out_ctx);
+moe_status moe_kv_destroy(moe_kv_ctx *ctx);
+
+/*
+ * Writes the new tokens' keys and values into their slots.  k, v: T rows of kv_heads * dim elements, ldk and ldv elements apart
+ * (views of one fused projection, say).  Strides are at least kv_heads * dim and rows are 16-byte aligned.  MOE_KV_FP8: the
+ * scale of a token and head is 2^e with the smallest e >= -100 for which amax <= 448 * 2^e (2^-9 for a row of zeros), the codes are the values over it, rounded
+ * to nearest even; a row with a value that is not finite gets the scale byte 255 and NaN codes.  Two rows that share a slot (a
+ * page listed twice) leave either's values.
+ */
+moe_status moe_kv_append(moe_kv_ctx *ctx, const void *k, int64_t ldk, const void *v, int64_t ldv, int64_t T,
+                         const moe_kv_pages *pages, const moe_kv_batch *batch, void *stream);
+
+/* Reads the rows' keys and values back: k, v as for moe_kv_append, here written, in dtype (rounded once). */
+moe_status moe_kv_gather(moe_kv_ctx *ctx, const moe_kv_pages *pages, const moe_kv_batch *batch, int64_t T, void *k, int64_t ldk,
+                         void *v, int64_t ldv, void *stream);
+
+typedef struct {
+    int32_t causal;     /* 1: a row at position p sees tokens 0 .. p; 0: all of its sequence */
+    int32_t window;     /* > 0: only tokens from p - window + 1 on; 0: no window */
+    const float *sinks; /* [heads] fp32 (device) or NULL: a logit per head that joins the softmax's sum without a value */
+} moe_attention_options;
+
+/*
+ * Attention of the T new rows to what their sequences hold (the new tokens' keys and values are appended first):
+ *   z_j = q . k_j / sqrt(dim) for the tokens j that the row sees, w = softmax over z (and the head's sink),
+ *   out = sum_j w_j v_j,   lse = ln(sum_j e^z_j) (the sink included), for joining parts of a history.
+ * q, out: T rows of heads * dim elements, ldq and ldo apart; lse [T, heads] fp32 or NULL.  A row that sees nothing gives zeros,
+ * and the sink (or minus infinity) as its lse.  bf16 contexts multiply on the matrix cores with fp32 sums, the weights w rounded
+ * to bf16 against the maximum; maxima, sums and partial outputs are fp32.  What a row does not see has no part in its result,
+ * whatever it holds.  The result of a row is the same bits for the same batch; it may differ in rounding with the other
+ * sequences of the batch, because long histories are split among compute units by the batch's total work.
+ */
+moe_status moe_paged_attention(moe_kv_ctx *ctx, const void *q, int64_t ldq, int64_t T, const moe_kv_pages *pages,
+                               const moe_kv_batch *batch, const moe_attention_options *opt, void *out, int64_t ldo, float *lse,
+                               void *stream);
+
 const char *moe_status_string(moe_status s);
 
 #ifdef __cplusplus

@@ -18,13 +18,16 @@ _lib = None
 MOE_F32, MOE_BF16 = 0, 1
 MOE_SCHED_CHUNKED, MOE_SCHED_LAYERED = 0, 1
 MOE_W_DTYPE, MOE_W_MXFP4 = 0, 1
+MOE_KV_DTYPE, MOE_KV_FP8 = 0, 1
+KV_FORMATS = {"": MOE_KV_DTYPE, "dtype": MOE_KV_DTYPE, "fp8": MOE_KV_FP8}
 WEIGHT_FORMATS = {"": MOE_W_DTYPE, "dtype": MOE_W_DTYPE, "mxfp4": MOE_W_MXFP4}
 
 EXPORTS = ["moe_workspace_bytes", "moe_create", "moe_destroy", "moe_router_topk", "moe_router_topk_noalloc", "moe_permute",
            "moe_grouped_ffn", "moe_grouped_ffn_mxfp4", "moe_combine", "moe_group_forward", "moe_num_layer_groups", "moe_layer_groups",
            "moe_stack_forward", "moe_read_counters", "moe_reset_counters",
            "moe_kernel_timing", "moe_read_kernel_timing", "moe_ffn_variant", "moe_set_ffn_variant",
-           "moe_status_string"]
+           "moe_status_string", "moe_kv_workspace_bytes", "moe_kv_create", "moe_kv_destroy", "moe_kv_append", "moe_kv_gather",
+           "moe_paged_attention"]
 
 FFN_VARIANTS = {"auto": 0, "tile128": 1, "small": 2, "big": 3, "w4_tile64": 4, "w4_stream": 5, "w4_big": 6, "few": 7, "wide": 8}
 
@@ -62,6 +65,25 @@ class CCounters(ctypes.Structure):
     _fields_ = [("expert_bytes", ctypes.c_uint64), ("router_bytes", ctypes.c_uint64),
                 ("active_experts_total", ctypes.c_uint64), ("tokens_processed", ctypes.c_uint64),
                 ("iterations", ctypes.c_uint32), ("layer_passes", ctypes.c_uint32)]
+
+
+class CKVConfig(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("kv_format", ctypes.c_int32)]
+
+
+class CKVPages(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("n_pages", ctypes.c_int64)]
+
+
+class CKVBatch(ctypes.Structure):
+    _fields_ = [("row_offsets", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("n_seqs", ctypes.c_int64), ("max_pages", ctypes.c_int64)]
+
+
+class CAttentionOptions(ctypes.Structure):
+    _fields_ = [("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_void_p)]
 
 
 @dataclass
@@ -104,6 +126,13 @@ def load():
     L.moe_ffn_variant.argtypes = [vp, i64]
     L.moe_ffn_variant.restype = ctypes.c_char_p
     L.moe_set_ffn_variant.argtypes = [vp, i32]
+    pages, batch = ctypes.POINTER(CKVPages), ctypes.POINTER(CKVBatch)
+    L.moe_kv_workspace_bytes.argtypes = [ctypes.POINTER(CKVConfig), ctypes.POINTER(ctypes.c_size_t)]
+    L.moe_kv_create.argtypes = [ctypes.POINTER(CKVConfig), vp, ctypes.c_size_t, ctypes.POINTER(vp)]
+    L.moe_kv_destroy.argtypes = [vp]
+    L.moe_kv_append.argtypes = [vp, vp, i64, vp, i64, i64, pages, batch, vp]
+    L.moe_kv_gather.argtypes = [vp, pages, batch, i64, vp, i64, vp, i64, vp]
+    L.moe_paged_attention.argtypes = [vp, vp, i64, i64, pages, batch, ctypes.POINTER(CAttentionOptions), vp, i64, vp, vp]
     L.moe_status_string.argtypes = [i32]
     L.moe_status_string.restype = ctypes.c_char_p
     for name in EXPORTS:
@@ -329,3 +358,133 @@ class Context:
         """Pin the grouped-GEMM kernel shape of this context (a name of FFN_VARIANTS, or the id)."""
         v = FFN_VARIANTS[variant] if isinstance(variant, str) else int(variant)
         _check(self.lib.moe_set_ffn_variant(self._ctx, v), "moe_set_ffn_variant")
+
+
+def kv_workspace_bytes(heads, kv_heads, dim, page, dtype, kv_format="") -> int:
+    cfg = CKVConfig(heads, kv_heads, dim, page, _dtype_code(dtype), KV_FORMATS[kv_format])
+    out = ctypes.c_size_t(0)
+    _check(load().moe_kv_workspace_bytes(ctypes.byref(cfg), ctypes.byref(out)), "moe_kv_workspace_bytes")
+    return out.value
+
+
+class KVPages(CKVPages):
+    """The pages of one layer (moe_kv_pages); keeps their tensors alive."""
+    tensors = ()
+
+
+class KVBatch(CKVBatch):
+    """A batch's descriptors (moe_kv_batch); keeps their tensors alive."""
+    tensors = ()
+
+
+class KVContext:
+    """A moe_kv_ctx plus the torch-allocated workspace it lives on: a paged key/value cache's format and its attention.
+
+    Tensors of rows (q, k, v and what comes back) are [T, heads, dim] with any stride between rows, so views of one fused
+    projection can be handed over.  The struct of a batch holds pointers only: what its tensors hold when a call runs counts."""
+
+    def __init__(self, heads, kv_heads, dim, page, dtype=torch.bfloat16, kv_format="", device="cuda:0"):
+        self.lib = load()
+        self.heads, self.kv_heads, self.dim, self.page = heads, kv_heads, dim, page
+        self.dtype = dtype
+        self.kv_format = kv_format
+        self.device = torch.device(device)
+        self.cfg = CKVConfig(heads, kv_heads, dim, page, _dtype_code(dtype), KV_FORMATS[kv_format])
+        self.fp8 = self.cfg.kv_format == MOE_KV_FP8
+        self.page_dtype = torch.float8_e4m3fn if self.fp8 else dtype
+        n = ctypes.c_size_t(0)
+        _check(self.lib.moe_kv_workspace_bytes(ctypes.byref(self.cfg), ctypes.byref(n)), "moe_kv_workspace_bytes")
+        self.workspace = torch.empty(n.value + 256, dtype=torch.uint8, device=self.device)
+        base = (self.workspace.data_ptr() + 255) // 256 * 256
+        self._ctx = ctypes.c_void_p()
+        _check(self.lib.moe_kv_create(ctypes.byref(self.cfg), ctypes.c_void_p(base), n.value, ctypes.byref(self._ctx)), "moe_kv_create")
+
+    def close(self):
+        if self._ctx:
+            self.lib.moe_kv_destroy(self._ctx)
+            self._ctx = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _stream(self):
+        if self.device.type != "cuda":
+            raise ValueError(f"the kernels run on a GPU, not on {self.device}")
+        return _stream()
+
+    def _dense(self, t, name, dtype, shape):
+        if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != self.workspace.device:
+            raise ValueError(f"{name}: a contiguous {dtype} tensor {shape} on {self.workspace.device} is needed, "
+                             f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def _rows(self, t, name, T, heads):
+        """Pointer and row stride of a [T, heads, dim] tensor."""
+        if t.shape != (T, heads, self.dim) or t.dtype != self.dtype or t.device != self.workspace.device:
+            raise ValueError(f"{name}: a {self.dtype} tensor {(T, heads, self.dim)} on {self.workspace.device} is needed, "
+                             f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+        ld, head, one = t.stride()
+        if (one != 1 and self.dim > 1) or (head != self.dim and heads > 1):
+            raise ValueError(f"{name}: a row's heads must lie side by side, not with strides {t.stride()}")
+        return t.data_ptr(), (ld if T > 1 else heads * self.dim)
+
+    def pack_pages(self, k_pages, v_pages, k_scales=None, v_scales=None) -> KVPages:
+        """The struct of a layer's pages [n_pages, kv_heads, page, dim] (and scales [n_pages, kv_heads, page] of FP8 ones)."""
+        n = k_pages.shape[0]
+        shape = (n, self.kv_heads, self.page, self.dim)
+        p = KVPages(self._dense(k_pages, "k_pages", self.page_dtype, shape), self._dense(v_pages, "v_pages", self.page_dtype, shape),
+                    None, None, n)
+        if self.fp8:
+            if k_scales is None or v_scales is None:
+                raise ValueError("FP8 pages need k_scales and v_scales")
+            p.k_scales = self._dense(k_scales, "k_scales", torch.uint8, shape[:3])
+            p.v_scales = self._dense(v_scales, "v_scales", torch.uint8, shape[:3])
+        elif k_scales is not None or v_scales is not None:
+            raise ValueError("scales belong to FP8 pages")
+        p.tensors = (k_pages, v_pages, k_scales, v_scales)
+        return p
+
+    def pack_batch(self, row_offsets, kv_lens, page_table) -> KVBatch:
+        """The struct of a batch's descriptors: row_offsets [n_seqs + 1], kv_lens [n_seqs], page_table [n_seqs, max_pages], int32."""
+        n = kv_lens.shape[0]
+        b = KVBatch(self._dense(row_offsets, "row_offsets", torch.int32, (n + 1,)), self._dense(kv_lens, "kv_lens", torch.int32, (n,)),
+                    self._dense(page_table, "page_table", torch.int32, (n, page_table.shape[1])), n, page_table.shape[1])
+        b.tensors = (row_offsets, kv_lens, page_table)
+        return b
+
+    # ---- the calls of the boundary, same names as the C ABI ----
+
+    def moe_kv_append(self, k, v, pages, batch):
+        T = k.shape[0]
+        kp, ldk = self._rows(k, "k", T, self.kv_heads)
+        vp, ldv = self._rows(v, "v", T, self.kv_heads)
+        _check(self.lib.moe_kv_append(self._ctx, kp, ldk, vp, ldv, T, pages, batch, self._stream()), "moe_kv_append")
+
+    def moe_kv_gather(self, pages, batch, T=None, k=None, v=None):
+        """The rows' keys and values [T, kv_heads, dim]; T: the batch's rows, needed where no outputs are passed in."""
+        if k is None or v is None:
+            T = T if T is not None else (k if k is not None else v).shape[0]
+            made = [torch.empty((T, self.kv_heads, self.dim), dtype=self.dtype, device=self.device) for t in (k, v) if t is None]
+            k = made.pop() if k is None else k
+            v = made.pop() if v is None else v
+        T = k.shape[0]
+        kp, ldk = self._rows(k, "k", T, self.kv_heads)
+        vp, ldv = self._rows(v, "v", T, self.kv_heads)
+        _check(self.lib.moe_kv_gather(self._ctx, pages, batch, T, kp, ldk, vp, ldv, self._stream()), "moe_kv_gather")
+        return k, v
+
+    def moe_paged_attention(self, q, pages, batch, causal=True, window=0, sinks=None, out=None, lse=None):
+        """out [T, heads, dim]; lse: a [T, heads] fp32 tensor to receive the rows' log-sum-exp, or None."""
+        T = q.shape[0]
+        if out is None:
+            out = torch.empty((T, self.heads, self.dim), dtype=self.dtype, device=self.device)
+        qp, ldq = self._rows(q, "q", T, self.heads)
+        op, ldo = self._rows(out, "out", T, self.heads)
+        opt = CAttentionOptions(int(bool(causal)), int(window),
+                                self._dense(sinks, "sinks", torch.float32, (self.heads,)) if sinks is not None else None)
+        lp = self._dense(lse, "lse", torch.float32, (T, self.heads)) if lse is not None else None
+        _check(self.lib.moe_paged_attention(self._ctx, qp, ldq, T, pages, batch, opt, op, ldo, lp, self._stream()), "moe_paged_attention")
+        return out

@@ -1,0 +1,52 @@
+// Shared by the kernels of the paged key/value cache (kv_cache.hip) and its attention (attention.hip).
+#pragma once
+#include "common.h"
+
+namespace moe {
+
+// A layer's pages and a batch's descriptors as the kernels take them.  Everything that comes from the descriptors is clamped or
+// tested on the device before it becomes an address.
+struct KVView {
+    char *k, *v;
+    uint8_t *ks, *vs;              // NULL unless the pages hold FP8 codes
+    const int32_t *off, *lens, *table;
+    int n_pages, S, max_pages;
+    int T, Hk, D, page_shift;
+};
+
+// The 64-bit index of a token's row among the rows of all pages, [n_pages, Hk, page].
+__device__ __forceinline__ int64_t page_row(int id, int Hk, int h, int shift, int slot)
+{
+    return ((((int64_t)id * Hk) + h) << shift) + slot;
+}
+
+// The factor that a scale byte stands for.
+__device__ __forceinline__ float scale_of(uint32_t byte)
+{
+    const float f = __builtin_amdgcn_ldexpf(1.0f, (int)byte - 127);
+    return byte == 255u ? __builtin_nanf("") : f;
+}
+
+// kv_cache.hip
+hipError_t launch_kv_append(int dtype, bool fp8, const KVView& c, const void* k, int64_t ldk, const void* v, int64_t ldv, hipStream_t s);
+hipError_t launch_kv_gather(int dtype, bool fp8, const KVView& c, void* k, int64_t ldk, void* v, int64_t ldv, hipStream_t s);
+
+// attention.hip
+struct AttnArgs {
+    KVView c;
+    const void* q;
+    void* out;
+    float* lse;
+    const float* sinks;
+    int64_t ldq, ldo;
+    int Hq, G, causal, window;
+    int tile_rows;                 // packed rows of a tile, where a sequence has more than 16 (set by launch_attention)
+    float scale2;                  // log2(e) / sqrt(dim): scores are kept as powers of two
+    float* part;                   // partial outputs, kPartUnits of 16 rows x D
+    float2* part_stats;            // and their rows' maximum and sum
+};
+// Partial results are stored in units of 16 rows.
+constexpr int kPartUnits = 4096;
+hipError_t launch_attention(int dtype, bool fp8, AttnArgs a, hipStream_t s);
+
+}  // namespace moe
