@@ -44,7 +44,7 @@ def _scratch_users(log, names):
 # load).  The compiler does not honour an M0 clobber on an asm statement, so these files must hold no other
 # use of M0; the build reads the device assembly (a by-product of the same compile) and checks that M0
 # only ever appears as  s_mov_b32 m0, <sgpr> ; s_nop 0 ; global_load_lds_<size>.
-M0_ONLY_FOR_LDS_LOADS = ("ffn.hip", "ffn_w4.hip")
+M0_ONLY_FOR_LDS_LOADS = ("ffn.hip", "ffn_w4.hip", "attention.hip")
 
 
 def _foreign_m0_uses(asm):

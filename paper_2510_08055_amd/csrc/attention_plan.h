@@ -1,0 +1,394 @@
+// What the attention's kernels share: the plan that finds a block's work, and how finished rows are stored.
+#pragma once
+#include <cfloat>
+
+#include "kv.h"
+
+namespace moe {
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
+typedef float float16_t __attribute__((ext_vector_type(16)));
+
+constexpr float kLowest = -FLT_MAX;      // a running maximum before its first token: finite, so that no difference is NaN
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// Items that the pieces of a launch aim at, of each kind of tile.  Pieces are no shorter than kMinPiece tokens (a step of 32 for each
+// of a block's four waves) or kMinTilePiece.
+constexpr int kFewItems = 2048, kTileItems = 512;
+constexpr int kMinPiece = 128, kMinTilePiece = 256;
+
+struct Seq {
+    int row0, n, kv;                // first row, rows, tokens held
+    int tiles, units, len;          // tiles of packed rows, units of 16 rows to a tile, tokens of the longest tile's range
+    bool many;                      // its tiles are those of attention_tile.h
+};
+struct Item {
+    Seq q;
+    int seq, head, tile, sub;       // sub: the piece
+    int piece;                      // tokens of a piece; 0: the history is in one
+    int slot;                       // of the partial results: first unit of the tile's first piece
+    bool valid;
+};
+
+__device__ __forceinline__ Seq shape_of(const AttnArgs& a, int lo, int hi, int kv)
+{
+    Seq q;
+    lo = lo < 0 ? 0 : (lo > a.c.T ? a.c.T : lo);
+    hi = hi < lo ? lo : (hi > a.c.T ? a.c.T : hi);
+    const int most = a.c.max_pages << a.c.page_shift;
+    q.row0 = lo;
+    q.n = hi - lo;
+    q.kv = kv < 0 ? 0 : (kv > most ? most : kv);
+    const int rows = q.n * a.G;
+    q.many = rows > a.few_rows && a.tile_rows > a.few_rows;
+    const int per = rows <= 16 ? 16 : rows <= a.few_rows ? a.few_rows : a.tile_rows;
+    q.units = per / 16;
+    q.tiles = (rows + per - 1) / per;
+    q.len = q.kv;
+    if (a.window > 0) {
+        const int first = q.kv - q.n - a.window + 1;
+        int len = q.kv - (first > 0 ? first : 0) + 31;
+        const int one = a.window + per / a.G + 2 + 31;       // (windows are at most 2^30)
+        if (a.causal && one < len) len = one;
+        if (len < q.len) q.len = len;
+    }
+    return q;
+}
+
+__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
+__device__ __forceinline__ float last_lane(float v) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63)); }
+
+// The largest of `first` and the values of the lanes below.
+__device__ __forceinline__ int wave_max_below(int v, int first)
+{
+    int x = __builtin_amdgcn_update_dpp(first, v, 0x138, 0xF, 0xF, false);      // the lane below's; lane 0: first
+    auto step = [&](auto ctrl, auto row_mask) {
+        const int o = __builtin_amdgcn_update_dpp(x, x, decltype(ctrl)::value, decltype(row_mask)::value, 0xF, false);
+        x = o > x ? o : x;
+    };
+    using std::integral_constant;
+    step(integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{});
+    step(integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{});
+    step(integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});
+    step(integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});
+    step(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});
+    step(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});
+    return x;
+}
+
+// The item of block `block`.  Sequences are taken 256 at a time, four to a lane.  Tiles of many rows come first: they take longest.
+// A sequence whose partial results no longer fit the workspace stays in one piece.
+__device__ __forceinline__ Item find_item(const AttnArgs& a, int block)
+{
+    const int lane = lane_id();
+    const int S = a.c.S, Hk = a.c.Hk;
+    Seq q[4];
+    int start = 0;                  // where the sequences before a load's end
+    auto load = [&](int b) {
+        if (b == 0) start = 0;
+        int off[5], kv[4];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) {
+            const int s = b + lane * 4 + i;
+            off[i] = a.c.off[s < S ? s : S];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int s = b + lane * 4 + i;
+            kv[i] = a.c.lens[s < S ? s : S - 1];
+        }
+        // Offsets that descend would name rows twice; a sequence starts no earlier than all before it have ended, so there are never more
+        // rows than T, nor more items than the launch has blocks.
+#pragma unroll
+        for (int i = 0; i < 4; ++i) off[i + 1] = off[i + 1] > off[i] ? off[i + 1] : off[i];
+        int before = wave_max_below(off[4], start);
+        start = last_lane(before > off[4] ? before : off[4]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int lo = before > off[i] ? before : off[i], hi = b + lane * 4 + i < S ? (before > off[i + 1] ? before : off[i + 1]) : lo;
+            q[i] = shape_of(a, lo, hi, kv[i]);
+        }
+    };
+    float few = 0, many = 0;
+    for (int b = 0; b < S; b += 256) {
+        load(b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float w = (float)q[i].tiles * (float)q[i].len;
+            (q[i].many ? many : few) += w;
+        }
+    }
+    few = last_lane(wave_scan(few)) * (float)Hk;
+    many = last_lane(wave_scan(many)) * (float)Hk;
+    // A token costs an item of either kind about the same time (of a unit's share of the memory, or of its matrix cores).
+    auto even = [](float work, int items, int least) {
+        const float v = work * (1.0f / (float)items);
+        return v <= (float)least ? least : v < 1e9f ? ((int)v + least) / least * least : 1 << 30;
+    };
+    const int few_piece = even(few, kFewItems, kMinPiece), many_piece = even(few + many, kTileItems, kMinTilePiece);
+
+    Item it;
+    it.valid = false;
+    int items0 = 0;
+    for (int pass = many > 0 ? 0 : 1; pass < 2; ++pass) {
+        float slots0 = 0;           // (as floats: they only grow, and past the workspace only that counts)
+        for (int b = 0; b < S; b += 256) {
+            if (S > 256) load(b);
+            int pieces[4];
+            float need[4], want = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int piece = q[i].many ? many_piece : few_piece;
+                pieces[i] = q[i].len > piece ? (q[i].len + piece - 1) / piece : 1;
+                need[i] = pieces[i] > 1 ? (float)(q[i].tiles * q[i].units) * (float)(Hk * pieces[i]) : 0.0f;
+                want += need[i];
+            }
+            const float incl = wave_scan(want);
+            float at = slots0 + incl - want;
+            int mine = 0, slot[4], count[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                slot[i] = 0;
+                if (need[i] > 0) {
+                    if (at + need[i] <= (float)kPartUnits) slot[i] = (int)at;
+                    else pieces[i] = 1;
+                }
+                at += need[i];
+                count[i] = q[i].many == (pass == 0) ? q[i].tiles * Hk * pieces[i] : 0;
+                mine += count[i];
+            }
+            slots0 += last_lane(incl);
+            const int incl_items = items0 + wave_scan(mine);
+            const unsigned long long hit = __ballot(block < incl_items);
+            if (hit != 0) {
+                const int src = __ffsll((long long)hit) - 1;
+                int rem = block - (incl_items - mine);
+                int seq = 0, sl = 0, pc = 1;
+                Seq f = q[0];
+                bool found = false;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (!found && rem < count[i]) {
+                        found = true;
+                        f = q[i];
+                        seq = b + lane * 4 + i;
+                        sl = slot[i];
+                        pc = pieces[i];
+                    } else if (!found) {
+                        rem -= count[i];
+                    }
+                }
+                auto pick = [&](int v) { return __builtin_amdgcn_readlane(v, src); };
+                it.q.row0 = pick(f.row0); it.q.n = pick(f.n); it.q.kv = pick(f.kv);
+                it.q.tiles = pick(f.tiles); it.q.units = pick(f.units); it.q.len = pick(f.len);
+                it.q.many = pass == 0;
+                it.seq = pick(seq);
+                rem = pick(rem);
+                sl = pick(sl);
+                pc = pick(pc);
+                // heads side by side (they go to different XCDs, and the tiles of a head to the same ones), long tiles first
+                it.head = rem % Hk;
+                rem /= Hk;
+                it.sub = rem % pc;
+                it.tile = it.q.tiles - 1 - rem / pc;
+                it.piece = pc == 1 ? 0 : it.q.many ? many_piece : few_piece;
+                it.slot = sl + (it.tile * Hk + it.head) * pc * it.q.units;
+                it.valid = rem >= 0 && it.tile >= 0;      // (always, but for descriptors so wrong that the counts overflow)
+                return it;
+            }
+            items0 = last_lane(incl_items);
+        }
+    }
+    return it;
+}
+
+// The tokens that a tile's rows see: all rows those of [full_lo, full_hi), some row those of [lo, hi); lo is a multiple of 32.
+struct Range {
+    int p0;                         // position of the sequence's first row
+    int rows, first;                // packed rows of the sequence, the tile's first
+    int lo, hi, full_lo, full_hi;
+    int pieces;
+    int begin, end;                 // tokens of the item's piece
+};
+__device__ __forceinline__ Range range_of(const AttnArgs& a, const Item& it)
+{
+    Range r;
+    r.rows = it.q.n * a.G;
+    r.first = it.tile * it.q.units * 16;
+    const int end = r.first + it.q.units * 16;
+    const int last = (end < r.rows ? end : r.rows) - 1;
+    r.p0 = it.q.kv - it.q.n;
+    const int p_first = r.p0 + r.first / a.G, p_last = r.p0 + last / a.G;
+    r.hi = a.causal && p_last + 1 < it.q.kv ? p_last + 1 : it.q.kv;
+    if (r.hi < 0) r.hi = 0;
+    r.full_hi = a.causal && p_first + 1 < it.q.kv ? p_first + 1 : it.q.kv;
+    r.lo = a.window > 0 && p_first - a.window + 1 > 0 ? p_first - a.window + 1 : 0;
+    r.full_lo = a.window > 0 && p_last - a.window + 1 > 0 ? p_last - a.window + 1 : 0;
+    r.lo &= ~31;
+    const int len = r.hi > r.lo ? r.hi - r.lo : 0;
+    r.pieces = it.piece > 0 && len > it.piece ? (len + it.piece - 1) / it.piece : 1;
+    r.begin = r.lo;
+    r.end = r.hi;
+    if (r.pieces > 1) {
+        r.begin += it.sub * it.piece;
+        if (r.end - r.begin > it.piece) r.end = r.begin + it.piece;
+    }
+    return r;
+}
+
+// What a packed row sees and where it lives.
+struct Row {
+    bool there;
+    int row, head;                  // of the batch, of the queries
+    int see_lo, see_hi;             // tokens [see_lo, see_hi)
+};
+__device__ __forceinline__ Row row_of(const AttnArgs& a, const Item& it, const Range& rg, int r)
+{
+    Row x;
+    x.there = r < rg.rows;
+    const int tok = x.there ? r / a.G : 0;
+    x.row = it.q.row0 + tok;
+    x.head = it.head * a.G + (x.there ? r - tok * a.G : 0);
+    const int p = rg.p0 + tok;
+    x.see_hi = !x.there ? 0 : (a.causal && p + 1 < it.q.kv ? p + 1 : it.q.kv);
+    x.see_lo = a.window > 0 ? p - a.window + 1 : 0;
+    return x;
+}
+
+// Entries of a sequence's page table, 64 at a time, one to a lane; an entry that names no page, or lies past `end`, is -1.
+struct Entries {
+    int base = 0, id = -1;
+    __device__ __forceinline__ void hold(const KVView& c, int seq, int page, int end)
+    {
+        base = page;
+        const int p = page + lane_id();
+        int v = -1;
+        if (p < c.max_pages && ((int64_t)p << c.page_shift) < end) v = c.table[(int64_t)seq * c.max_pages + p];
+        id = v >= 0 && v < c.n_pages ? v : -1;
+    }
+};
+
+// N consecutive dwords, as wide as they can be loaded.
+template <int N> __device__ __forceinline__ void load_dwords(const char* p, uint32_t (&x)[N])
+{
+    if constexpr (N == 1) {
+        x[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else if constexpr (N == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        x[0] = v.x; x[1] = v.y;
+    } else {
+        static_assert(N % 4 == 0, "whole 16-byte pieces");
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+            x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+        }
+    }
+}
+
+// What turns a row's sums into its result: the factor of its outputs, and its log-sum-exp.
+struct Finish {
+    float factor, lse;
+};
+__device__ __forceinline__ Finish finish_row(const AttnArgs& a, int head, float m, float l)
+{
+    Finish f;
+    f.factor = 1.0f;
+    if (a.sinks) {
+        const float s2 = a.sinks[head] * kLog2e;
+        const float m2 = fmaxf(m, s2);
+        f.factor = __builtin_amdgcn_exp2f(m - m2);
+        l = l * f.factor + __builtin_amdgcn_exp2f(s2 - m2);
+        m = m2;
+    }
+    f.factor = l == 0.0f ? 0.0f : f.factor / l;
+    f.lse = l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    return f;
+}
+// Four dimensions from d on of a finished row.
+template <typename T> __device__ __forceinline__ void store_out(const AttnArgs& a, int row, int head, int d, float4 o)
+{
+    T* dst = static_cast<T*>(a.out) + (int64_t)row * a.ldo + head * a.c.D + d;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
+    else *reinterpret_cast<float4*>(dst) = o;
+}
+
+// ---- partial results of a piece: per row its output sums, maximum and sum, to be read by the block that ends the tile ----
+__device__ __forceinline__ uint64_t two(float x, float y) { return (uint64_t)__float_as_uint(x) | (uint64_t)__float_as_uint(y) << 32; }
+__device__ __forceinline__ float2 two_of(uint64_t v) { return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))); }
+__device__ __forceinline__ void store_part(const AttnArgs& a, int64_t row, int d, float4 o)
+{
+    uint64_t* dst = reinterpret_cast<uint64_t*>(a.part + row * a.c.D + d);
+    store_shared(dst, two(o.x, o.y));
+    store_shared(dst + 1, two(o.z, o.w));
+}
+__device__ __forceinline__ void store_part_stats(const AttnArgs& a, int64_t row, float m, float l)
+{
+    store_shared(reinterpret_cast<uint64_t*>(a.part_stats + row), two(m, l));
+}
+
+// Every thread of a block that has stored its piece of a tile calls it; the block that ends the tile joins its pieces, in their order (so
+// the result does not depend on who came last).  Sixteen lanes to a row, four pieces in flight.
+template <typename T, int DP> __device__ __forceinline__ void join_pieces(const AttnArgs& a, const Item& it, const Range& rg, int32_t* flag)
+{
+    if (!last_to_arrive(a.tickets + it.slot, (uint32_t)rg.pieces, flag)) return;
+    constexpr int ND = (DP + 63) / 64;
+    const int units = it.q.units, D = a.c.D, d0 = (threadIdx.x & 15) * 4;
+    for (int u = 0; u < units; ++u) {
+        const int q = threadIdx.x >> 4, r = rg.first + u * 16 + q;
+        if (r >= rg.rows) return;
+        float M = kLowest, L = 0;
+        float4 o[ND];
+#pragma unroll
+        for (int k = 0; k < ND; ++k) o[k] = make_float4(0, 0, 0, 0);
+        for (int c0 = 0; c0 < rg.pieces; c0 += 4) {
+            float2 st[4];
+            uint64_t x[4][ND][2];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int at = c0 + c < rg.pieces ? c0 + c : rg.pieces - 1;
+                const int64_t row = (int64_t)(it.slot + at * units + u) * 16 + q;
+                st[c] = two_of(load_shared(reinterpret_cast<const uint64_t*>(a.part_stats + row)));
+#pragma unroll
+                for (int k = 0; k < ND; ++k) {
+                    const uint64_t* src = reinterpret_cast<const uint64_t*>(a.part + row * D + (d0 + k * 64 < D ? d0 + k * 64 : 0));
+                    x[c][k][0] = load_shared(src);
+                    x[c][k][1] = load_shared(src + 1);
+                }
+            }
+            float top = M;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) top = fmaxf(top, st[c].x);
+            const float back = __builtin_amdgcn_exp2f(M - top);
+            M = top;
+            L *= back;
+#pragma unroll
+            for (int k = 0; k < ND; ++k) { o[k].x *= back; o[k].y *= back; o[k].z *= back; o[k].w *= back; }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if (c0 + c < rg.pieces) {
+                    const float f = __builtin_amdgcn_exp2f(st[c].x - top);
+                    L += st[c].y * f;
+#pragma unroll
+                    for (int k = 0; k < ND; ++k) {
+                        const float2 lo = two_of(x[c][k][0]), hi = two_of(x[c][k][1]);
+                        o[k].x += lo.x * f; o[k].y += lo.y * f; o[k].z += hi.x * f; o[k].w += hi.y * f;
+                    }
+                }
+            }
+        }
+        const Row row = row_of(a, it, rg, r);
+        const Finish f = finish_row(a, row.head, M, L);
+#pragma unroll
+        for (int k = 0; k < ND; ++k)
+            if (d0 + k * 64 < D)
+                store_out<T>(a, row.row, row.head, d0 + k * 64, make_float4(o[k].x * f.factor, o[k].y * f.factor, o[k].z * f.factor, o[k].w * f.factor));
+        if (a.lse && d0 == 0) a.lse[(int64_t)row.row * a.Hq + row.head] = f.lse;
+    }
+}
+
+}  // namespace
+}  // namespace moe

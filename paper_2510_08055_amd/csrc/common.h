@@ -64,6 +64,32 @@ template <typename V> __device__ __forceinline__ V wave_scan(V v)
     return v;
 }
 
+// Stores and loads that meet at the level every block of the launch sees (past the caches of one XCD), for data
+// that one block hands to another inside a launch; the order between them comes from the ticket counters.
+template <typename V> __device__ __forceinline__ void store_shared(V* p, V v)
+{
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename V> __device__ __forceinline__ V load_shared(const V* p)
+{
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Draws a ticket for the block once everything it has stored is visible; true for the last of n drawers.
+// Every thread of the block calls it (`flag`: a word of LDS).
+__device__ __forceinline__ bool last_to_arrive(uint32_t* ticket, uint32_t n, int32_t* flag)
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // this wave's stores have reached the shared level
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const bool last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == n - 1;
+        if (last) store_shared(ticket, 0u);
+        *flag = last;
+    }
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(*flag) != 0;
+}
+
 // A batch of rows that lives in two buffers: rows [0, n0) in p0, the rest in p1 (row t - n0).  The
 // layer-group driver reads the first layer's input straight from x_decode / x_prefill this way instead
 // of copying the two pieces together first.

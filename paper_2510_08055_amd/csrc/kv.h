@@ -40,13 +40,14 @@ struct AttnArgs {
     const float* sinks;
     int64_t ldq, ldo;
     int Hq, G, causal, window;
-    int tile_rows;                 // packed rows of a tile, where a sequence has more than 16 (set by launch_attention)
+    int few_rows, tile_rows;       // packed rows of a tile, up to few_rows and where a sequence has more (set by the launch)
     float scale2;                  // log2(e) / sqrt(dim): scores are kept as powers of two
     float* part;                   // partial outputs, kPartUnits of 16 rows x D
     float2* part_stats;            // and their rows' maximum and sum
+    uint32_t* tickets;             // kPartUnits, zero between launches
 };
 // Partial results are stored in units of 16 rows.
-constexpr int kPartUnits = 4096;
-hipError_t launch_attention(int dtype, bool fp8, AttnArgs a, hipStream_t s);
+constexpr int kPartUnits = 8192;
+hipError_t launch_attention(int dtype, bool fp8, const AttnArgs& a, hipStream_t s);
 
 }  // namespace moe

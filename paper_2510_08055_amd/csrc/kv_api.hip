@@ -11,6 +11,8 @@ struct moe_kv_ctx {
     moe_kv_config cfg;
     float* part;
     float2* part_stats;
+    uint32_t* tickets;
+    bool tickets_clear;
 };
 
 namespace {
@@ -31,6 +33,7 @@ moe_status check_cfg(const moe_kv_config* c)
 
 inline size_t part_bytes(const moe_kv_config& c) { return (size_t)kPartUnits * 16 * c.dim * sizeof(float); }
 inline size_t stats_bytes() { return (size_t)kPartUnits * 16 * sizeof(float2); }
+inline size_t workspace_size(const moe_kv_config& c) { return part_bytes(c) + stats_bytes() + kPartUnits * sizeof(uint32_t); }
 
 inline bool misaligned(const void* p, uintptr_t to = 16) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 inline moe_status dev(hipError_t e) { return e == hipSuccess ? MOE_OK : MOE_ERR_DEVICE; }
@@ -89,7 +92,7 @@ moe_status moe_kv_workspace_bytes(const moe_kv_config* cfg, size_t* out_bytes)
     if (!out_bytes) return MOE_ERR_NULL;
     const moe_status st = check_cfg(cfg);
     if (st != MOE_OK) return st;
-    *out_bytes = part_bytes(*cfg) + stats_bytes();
+    *out_bytes = workspace_size(*cfg);
     return MOE_OK;
 }
 
@@ -99,12 +102,14 @@ moe_status moe_kv_create(const moe_kv_config* cfg, void* workspace, size_t works
     const moe_status st = check_cfg(cfg);
     if (st != MOE_OK) return st;
     if (reinterpret_cast<uintptr_t>(workspace) % kAlign) return MOE_ERR_ALIGN;
-    if (workspace_bytes < part_bytes(*cfg) + stats_bytes()) return MOE_ERR_WORKSPACE;
+    if (workspace_bytes < workspace_size(*cfg)) return MOE_ERR_WORKSPACE;
     moe_kv_ctx* c = new (std::nothrow) moe_kv_ctx();
     if (!c) return MOE_ERR_DEVICE;
     c->cfg = *cfg;
     c->part = static_cast<float*>(workspace);
     c->part_stats = reinterpret_cast<float2*>(static_cast<char*>(workspace) + part_bytes(*cfg));
+    c->tickets = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + part_bytes(*cfg) + stats_bytes());
+    c->tickets_clear = false;
     *out_ctx = c;
     return MOE_OK;
 }
@@ -166,7 +171,20 @@ moe_status moe_paged_attention(moe_kv_ctx* ctx, const void* q, int64_t ldq, int6
     a.scale2 = (float)(1.4426950408889634 / std::sqrt((double)g.dim));
     a.part = ctx->part;
     a.part_stats = ctx->part_stats;
-    return dev(launch_attention(g.dtype, g.kv_format == MOE_KV_FP8, a, static_cast<hipStream_t>(stream)));
+    a.tickets = ctx->tickets;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (!ctx->tickets_clear) {
+        // The tickets are zero between launches once they have been cleared: in front of a context's first call.  A call that is
+        // being captured carries the clear along, runs when its graph is replayed, and so leaves it to the next call as well.
+        hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+        if (hipStreamIsCapturing(s, &capture) != hipSuccess) {
+            (void)hipGetLastError();        // (the legacy stream while another one is captured)
+            capture = hipStreamCaptureStatusActive;
+        }
+        if (launch_fill_zero(ctx->tickets, kPartUnits, s) != hipSuccess) return MOE_ERR_DEVICE;
+        ctx->tickets_clear = capture == hipStreamCaptureStatusNone;
+    }
+    return dev(launch_attention(g.dtype, g.kv_format == MOE_KV_FP8, a, s));
 }
 
 }  // extern "C"

@@ -111,32 +111,6 @@ __device__ __forceinline__ void wait_ring(vec8<float> (&x)[4], vec8<float> (&w)[
 // many blocks leaves a 20 % tail on 256 compute units, and the matrix pipe, not the loads, is the limit.)
 constexpr int kRouterBufs = 4;      // (wait_ring names exactly four buffers)
 
-// Stores and loads that meet at the level every block of the launch sees (past the caches of one XCD), for data
-// that one block hands to another inside a launch; the order between them comes from the ticket counters.
-template <typename V> __device__ __forceinline__ void store_shared(V* p, V v)
-{
-    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-template <typename V> __device__ __forceinline__ V load_shared(const V* p)
-{
-    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
-// Draws a ticket for the block once everything it has stored is visible; true for the last of n drawers.
-// Every thread of the block calls it (`flag`: a word of LDS).
-__device__ __forceinline__ bool last_to_arrive(uint32_t* ticket, uint32_t n, int32_t* flag)
-{
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // this wave's stores have reached the shared level
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        const bool last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == n - 1;
-        if (last) store_shared(ticket, 0u);
-        *flag = last;
-    }
-    __syncthreads();
-    return __builtin_amdgcn_readfirstlane(*flag) != 0;
-}
-
 // The tile of logits of rows row(0 .. 15) and experts e0 .. e0 + 15, stored by wave 0; every thread of the block calls it.
 // Rows from n_rows on are read and not used.  store(i, j, z) takes the logit z of row i < n_rows and expert e0 + j < E.
 template <typename T, int NW, typename Row, typename Store>
