@@ -18,6 +18,22 @@ namespace {
 // ----------------------------------------------------------------------------------------------------------------
 constexpr int kManyRows = 128;
 
+// N direct-to-LDS loads of a wave, 1 KB after the other in LDS and, but for what the offsets make good, in memory (the
+// instruction's offset counts in both): M0 is written once for all of them.
+constexpr uint32_t kGroupBias = 3072;        // keeps the 32-bit offsets from falling below zero
+template <int N> __device__ __forceinline__ void load_lds_group(const uint32_t (&off)[N], const char* base, uint32_t lds)
+{
+    if constexpr (N == 1)
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off[0]), "s"(base), "s"(lds) : "memory");
+    else if constexpr (N == 2)
+        asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024" ::"v"(off[0]),
+                     "v"(off[1]), "s"(base), "s"(lds) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024\n\t"
+                     "global_load_lds_dwordx4 %2, %4 offset:2048\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072" ::"v"(off[0]), "v"(off[1]),
+                     "v"(off[2]), "v"(off[3]), "s"(base), "s"(lds) : "memory");
+}
+
 template <bool FP8, int DP> struct Many {
     static constexpr int TOK = 64;
     static constexpr int ROWB = DP * 2;              // bytes of a token's row in LDS
@@ -46,10 +62,10 @@ template <bool FP8, int DP> struct Many {
         return __uint_as_float(x[0]) + __uint_as_float(x[1]);
     }
 
-    // The step's source in the cache: an address per group of 8 tokens (pages hold whole groups), and which groups are there.
+    // A step of 64 tokens; bit i of `there`: tokens t + 8 i .. t + 8 i + 7 are (pages hold whole groups of eight).
     struct Step {
         int t;
-        uint32_t there;              // bit i: tokens t + 8 i .. t + 8 i + 7
+        uint32_t there;
     };
 
     typedef short short4_t __attribute__((ext_vector_type(4)));
@@ -57,6 +73,11 @@ template <bool FP8, int DP> struct Many {
     static __device__ __forceinline__ uint2 read_transposed(uint32_t lds)
     {
         return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)(uintptr_t)lds));
+    }
+    typedef __attribute__((address_space(3))) const uint4 lds_uint4_t;
+    static __device__ __forceinline__ bf16x8_t read_keys(uint32_t lds)
+    {
+        return __builtin_bit_cast(bf16x8_t, *(lds_uint4_t*)(uintptr_t)lds);
     }
 
     static __device__ __forceinline__ void run(const AttnArgs& a, const Item& it, char* smem)
@@ -81,40 +102,60 @@ template <bool FP8, int DP> struct Many {
             }
         }
 
-        // ---- staging ----
+        // ---- staging: a wave's share of a step are 16 tokens, two groups of eight ----
+        // Per held entry of the page table, the byte offset of this head's first token in the pages (and its row, for the scales):
+        // a step then takes what it needs as scalars, and no lane works out an address.
         Entries pages;
-        const int64_t head_row = (int64_t)it.head << shift;
+        unsigned long long held = 0;
+        uint32_t byte_lo = 0, byte_hi = 0, row_lo = 0, row_hi = 0;
+        auto hold = [&](int page) {
+            pages.hold(a.c, it.seq, page, rg.end);
+            held = __ballot(pages.id >= 0);
+            const int64_t row = page_row(pages.id < 0 ? 0 : pages.id, Hk, it.head, shift, 0);
+            const int64_t byte = row * (D * (FP8 ? 1 : 2));
+            byte_lo = (uint32_t)byte;
+            byte_hi = (uint32_t)((uint64_t)byte >> 32);
+            row_lo = (uint32_t)row;
+            row_hi = (uint32_t)((uint64_t)row >> 32);
+        };
         auto step_at = [&](int t) {
-            if (((t + TOK - 1) >> shift) - pages.base >= 64) pages.hold(a.c, it.seq, t >> shift, rg.end);
-            const unsigned long long ok = __ballot(pages.id >= 0);
-            Step s;
-            s.t = t;
-            s.there = 0;
+            if (((t + TOK - 1) >> shift) - pages.base >= 64) hold(t >> shift);
+            const int first = (t >> shift) - pages.base, last = ((t + TOK - 1) >> shift) - pages.base;
+            Step s{t, 0xffu};
+            if ((~(held >> first) << (63 - (last - first))) != 0) {
+                s.there = 0;
 #pragma unroll
-            for (int i = 0; i < TOK / 8; ++i) s.there |= (uint32_t)((ok >> (((t + 8 * i) >> shift) - pages.base)) & 1) << i;
+                for (int i = 0; i < TOK / 8; ++i) s.there |= (uint32_t)((held >> (((t + 8 * i) >> shift) - pages.base)) & 1) << i;
+            }
             return s;
         };
-        // byte offset of token t's row (of a group of tokens that the wave shares) in the pages; row_bytes: of a cached row
-        auto group_row = [&](int t) {
-            int id = __builtin_amdgcn_readlane(pages.id, (t >> shift) - pages.base);
-            id = id < 0 ? 0 : id;
-            return ((((int64_t)id * Hk) << shift) + head_row + (t & ((1 << shift) - 1)));
+        auto lane64 = [](uint32_t lo, uint32_t hi, int i) {
+            return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)lo, i) |
+                             (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, i) << 32);
         };
-        // bf16: straight into LDS, 64 / CH tokens to a wave's load
-        constexpr int TPL = 64 / CH;
-        auto stage = [&](const Step& s, uint32_t base) {
+        const int mask = (1 << shift) - 1;
+        // bf16: straight into LDS, 64 / CH tokens to a load; the loads of a group follow each other in LDS
+        constexpr int TPL = 64 / CH, GL = LOADS / 2;
+        uint32_t from[2][GL];
+        if constexpr (!FP8) {
             const int tl = lane / CH, c = lane % CH;
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int t = (wave * LOADS + i) * TPL;              // of the step; the same 8-token group for all of the load
-                const int64_t row = group_row(s.t + t);
-                // (chunks past the dimension: keys meet zeros there, values go to outputs that are not stored)
-                const int chunk = c ^ swz(t + tl);
-                const uint32_t off = (uint32_t)(tl * D * 2 + (chunk * 8 < D ? chunk * 16 : 0));
-                const char* k = uniform(a.c.k + row * D * 2);
-                const char* v = uniform(a.c.v + row * D * 2);
-                load_lds_16_base(k, off, base + t * ROWB);
-                load_lds_16_base(v, off, base + HALF + t * ROWB);
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int i = 0; i < GL; ++i) {
+                    // (chunks past the dimension: keys meet zeros there, values go to outputs that are not stored)
+                    const int chunk = c ^ swz(g * 8 + i * TPL + tl);
+                    from[g][i] = (uint32_t)((i * TPL + tl) * D * 2 + (chunk * 8 < D ? chunk * 16 : 0) - i * 1024) + kGroupBias;
+                }
+        }
+        auto stage = [&](const Step& s, uint32_t base) {
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const int t = s.t + wave * 16 + g * 8;
+                const int64_t off = lane64(byte_lo, byte_hi, (t >> shift) - pages.base) + (t & mask) * (D * 2) - (int)kGroupBias;
+                const uint32_t to = base + (wave * 16 + g * 8) * ROWB;
+                load_lds_group(from[g], a.c.k + off, to);
+                load_lds_group(from[g], a.c.v + off, to + HALF);
             }
         };
         // FP8: 16 codes to a lane, through registers, widened exactly (a code has 4 significant bits, its scale is a power of two)
@@ -125,23 +166,30 @@ template <bool FP8, int DP> struct Many {
         uint32_t raw_scale[FP8 ? FL : 1][2];
         auto fetch = [&](const Step& s) {
             const int tl = lane / LPT, c = lane % LPT;
+            int64_t byte[2], row[2];
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const int t = s.t + wave * 16 + g * 8, i = (t >> shift) - pages.base;
+                byte[g] = lane64(byte_lo, byte_hi, i) + (t & mask) * D;
+                row[g] = lane64(row_lo, row_hi, i) + (t & mask);
+            }
 #pragma unroll
             for (int i = 0; i < FL; ++i) {
-                const int t = (wave * FL + i) * TPW + tl;
-                int id = __shfl(pages.id, ((s.t + t) >> shift) - pages.base);
-                const int64_t row = page_row(id < 0 ? 0 : id, Hk, it.head, shift, (s.t + t) & ((1 << shift) - 1));
-                const int64_t off = row * D + (c * 16 < D ? c * 16 : 0);
-                raw[i][0] = *reinterpret_cast<const uint4*>(a.c.k + off);
-                raw[i][1] = *reinterpret_cast<const uint4*>(a.c.v + off);
-                raw_scale[i][0] = a.c.ks[row];
-                raw_scale[i][1] = a.c.vs[row];
+                const int t = i * TPW + tl;            // of the wave's 16
+                const bool second = TPW > 8 ? t >= 8 : i * TPW >= 8;
+                const int64_t bb = second ? byte[1] : byte[0], rr = second ? row[1] : row[0];
+                const uint32_t off = (uint32_t)((t & 7) * D + (c * 16 < D ? c * 16 : 0));
+                raw[i][0] = *reinterpret_cast<const uint4*>(a.c.k + bb + off);
+                raw[i][1] = *reinterpret_cast<const uint4*>(a.c.v + bb + off);
+                raw_scale[i][0] = (a.c.ks + rr)[t & 7];
+                raw_scale[i][1] = (a.c.vs + rr)[t & 7];
             }
         };
         auto widen = [&](char* base) {
             const int tl = lane / LPT, c = lane % LPT;
 #pragma unroll
             for (int i = 0; i < FL; ++i) {
-                const int t = (wave * FL + i) * TPW + tl;
+                const int t = wave * 16 + i * TPW + tl;
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv) {
                     const float sc = scale_of(raw_scale[i][kv]);
@@ -159,16 +207,21 @@ template <bool FP8, int DP> struct Many {
             }
         };
 
-        // ---- operand addresses (relative to a stage) ----
-        // keys: token 32 b + n, chunk 2 s + h
-        const int k_row = n * ROWB, k_swz = swz(n);
-        // values: tokens 16 s + 8 u + 4 h + (lane % 16) / 4, dimensions 32 nb + 16 (lane / 16 % 2) + 4 (lane % 4): see read_transposed
-        const int v_tok = 4 * h + ((lane & 15) >> 2), v_chunk = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-        const int v_row = v_tok * ROWB + (lane & 1) * 8;
-        auto v_at = [&](int s, int u, int nb) {
-            const int t = 8 * u + v_tok;                             // (16 s does not change the swizzle)
-            return (uint32_t)(v_row + (16 * s + 8 * u) * ROWB + ((v_chunk + 4 * nb) ^ swz(t)) * 16);
-        };
+        // ---- operand addresses in the step's stage ----
+        // keys: token 32 b + n, chunk 2 c + h
+        uint32_t k_at[DP / 16];
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) k_at[c] = lds0 + n * ROWB + (((2 * c + h) ^ swz(n)) * 16);
+        // values: tokens 16 k + 8 u + 4 h + (lane % 16) / 4, dimensions 32 x + 16 (lane / 16 % 2) + 4 (lane % 4): see read_transposed
+        uint32_t v_at[2][NB];
+        {
+            const int tok = 4 * h + ((lane & 15) >> 2), chunk = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int x = 0; x < NB; ++x)
+                    v_at[u][x] = lds0 + HALF + (8 * u + tok) * ROWB + (lane & 1) * 8 + (((chunk + 4 * x) ^ swz(8 * u + tok)) * 16);
+        }
 
         float m = kLowest, l = 0;
         float16_t o[NB];
@@ -177,7 +230,7 @@ template <bool FP8, int DP> struct Many {
 
         Step cur{rg.begin, 0};
         if (rg.begin < rg.end) {
-            pages.hold(a.c, it.seq, rg.begin >> shift, rg.end);
+            hold(rg.begin >> shift);
             cur = step_at(rg.begin);
             if constexpr (FP8) {
                 fetch(cur);
@@ -187,7 +240,7 @@ template <bool FP8, int DP> struct Many {
             }
         }
         const bool idle = rg.first + wave * 32 >= rg.rows;           // a wave whose rows are none stages all the same
-        uint32_t at = 0;                                             // byte offset of the step's stage
+        int at = 0;                                                  // byte offset of the step's stage
         while (cur.t < rg.end) {
             if constexpr (FP8) wait_lds_reads();
             else wait_vmcnt<0>();
@@ -200,32 +253,31 @@ template <bool FP8, int DP> struct Many {
                 else stage(next, lds0 + (at ^ STAGE));
             }
             if (!idle) {
-                const char* kb = smem + at;
                 float16_t s[2];
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     s[b] = float16_t{};
 #pragma unroll
-                    for (int c = 0; c < DP / 16; ++c) {
-                        const uint4 kf = *reinterpret_cast<const uint4*>(kb + b * 32 * ROWB + k_row + (((2 * c + h) ^ k_swz) * 16));
-                        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf), qf[c], s[b], 0, 0, 0);
-                    }
+                    for (int c = 0; c < DP / 16; ++c)
+                        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_keys(k_at[c] + b * 32 * ROWB), qf[c], s[b], 0, 0, 0);
                 }
                 const bool masked = cur.t + TOK > rg.full_hi || cur.t < rg.full_lo || cur.there != 0xffu;
+                if (masked) {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int grp = b * 4 + r / 4, tok = cur.t + grp * 8 + 4 * h + r % 4;
+                            const bool sees = (((cur.there >> grp) & 1) != 0) & (tok < me.see_hi) & (tok >= me.see_lo);
+                            s[b][r] = sees ? s[b][r] : -__builtin_inff();
+                        }
+                }
                 float top = -__builtin_inff();
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        float x = s[b][r] * a.scale2;
-                        if (masked) {
-                            const int grp = b * 4 + r / 4, tok = cur.t + grp * 8 + 4 * h + r % 4;
-                            if (!(((cur.there >> grp) & 1) && tok < me.see_hi && tok >= me.see_lo)) x = -__builtin_inff();
-                        }
-                        s[b][r] = x;
-                        top = fmaxf(top, x);
-                    }
-                top = swap_max(top);
+                    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
+                top = swap_max(top) * a.scale2;                      // (the scale is positive)
                 // (the reference of the exponentials follows the maximum only when that has grown by more than 8, see attention_few.h)
                 if (__any(top > m + 8.0f)) {
                     const float to = fmaxf(top, m), f = __builtin_amdgcn_exp2f(m - to);
@@ -240,31 +292,38 @@ template <bool FP8, int DP> struct Many {
                     uint32_t u[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float p0 = __builtin_amdgcn_exp2f(s[k / 2][(k % 2) * 8 + 2 * i] - m);
-                        const float p1 = __builtin_amdgcn_exp2f(s[k / 2][(k % 2) * 8 + 2 * i + 1] - m);
+                        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k / 2][(k % 2) * 8 + 2 * i], a.scale2, -m));
+                        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k / 2][(k % 2) * 8 + 2 * i + 1], a.scale2, -m));
                         l += p0;
                         l += p1;
                         u[i] = pack_bf16x2(p0, p1);
                     }
                     w[k] = __builtin_bit_cast(bf16x8_t, make_uint4(u[0], u[1], u[2], u[3]));
                 }
-                const uint32_t vb = lds0 + at + HALF;
                 if (!masked) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
 #pragma unroll
                         for (int x = 0; x < NB; ++x) {
-                            const uint2 lo = read_transposed(vb + v_at(k, 0, x)), hi = read_transposed(vb + v_at(k, 1, x));
+                            const uint2 lo = read_transposed(v_at[0][x] + k * 16 * ROWB), hi = read_transposed(v_at[1][x] + k * 16 * ROWB);
                             o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                                 __builtin_bit_cast(bf16x8_t, make_uint4(lo.x, lo.y, hi.x, hi.y)), w[k], o[x], 0, 0, 0);
                         }
                 } else {
-                    careful_values(cur, rg, me, vb, v_at, w, o);
+                    careful_values(cur, rg, me, v_at, w, o);
                 }
             }
             if constexpr (FP8)
                 if (more) widen(smem + (at ^ STAGE));
-            at ^= STAGE;
+            const int turn = at == 0 ? STAGE : -STAGE;
+            at += turn;
+#pragma unroll
+            for (int c = 0; c < DP / 16; ++c) k_at[c] += turn;
+#pragma unroll
+            for (int x = 0; x < NB; ++x) {
+                v_at[0][x] += turn;
+                v_at[1][x] += turn;
+            }
             cur = next;
         }
 
@@ -299,8 +358,7 @@ template <bool FP8, int DP> struct Many {
     // The second product for a step whose tokens not every row sees: values of tokens that are not there, or that no row sees, are
     // zeros whatever the cache holds, and those that are not finite (a weight of zero would not keep them out) go to the rows
     // that see them as the infinity or NaN that they are.
-    template <typename At>
-    static __device__ __forceinline__ void careful_values(const Step& cur, const Range& rg, const Row& me, uint32_t vb, At v_at,
+    static __device__ __forceinline__ void careful_values(const Step& cur, const Range& rg, const Row& me, const uint32_t (&v_at)[2][NB],
                                                           const bf16x8_t (&w)[4], float16_t (&o)[NB])
     {
         const int h = lane_id() >> 5;
@@ -320,7 +378,7 @@ template <bool FP8, int DP> struct Many {
             }
 #pragma unroll
             for (int x = 0; x < NB; ++x) {
-                const uint2 lo = read_transposed(vb + v_at(k, 0, x)), hi = read_transposed(vb + v_at(k, 1, x));
+                const uint2 lo = read_transposed(v_at[0][x] + k * 16 * ROWB), hi = read_transposed(v_at[1][x] + k * 16 * ROWB);
                 uint32_t v[4] = {lo.x & keep[0], lo.y & keep[1], hi.x & keep[2], hi.y & keep[3]};
                 bool strange = false;
 #pragma unroll
