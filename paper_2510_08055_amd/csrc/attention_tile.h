@@ -40,7 +40,7 @@ template <bool FP8, int DP> struct Many {
     static constexpr int CH = DP / 8;                // its 16-byte chunks
     static constexpr int HALF = TOK * ROWB;          // keys, then values
     static constexpr int STAGE = 2 * HALF;
-    static constexpr size_t LDS = 2 * STAGE;
+    static constexpr size_t LDS = 2 * STAGE + 16;    // (and a flag)
     static constexpr int NB = DP / 32;               // output blocks of 32 dimensions
     static constexpr int LOADS = TOK * CH / 256;     // 16-byte loads of a thread for a step's keys (as many for its values)
 
@@ -74,10 +74,17 @@ template <bool FP8, int DP> struct Many {
     {
         return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)(uintptr_t)lds));
     }
-    typedef __attribute__((address_space(3))) const uint4 lds_uint4_t;
+    // Values of tokens 16 k .. 16 k + 15 in the order of the exponentials, dimensions 32 x .. 32 x + 31.
+    static __device__ __forceinline__ bf16x8_t read_values(const uint32_t (&v_at)[2][NB], int k, int x)
+    {
+        const uint2 lo = read_transposed(v_at[0][x] + k * 16 * ROWB), hi = read_transposed(v_at[1][x] + k * 16 * ROWB);
+        return __builtin_bit_cast(bf16x8_t, make_uint4(lo.x, lo.y, hi.x, hi.y));
+    }
+    typedef uint32_t uint32x4_t __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) uint32x4_t lds_chunk_t;
     static __device__ __forceinline__ bf16x8_t read_keys(uint32_t lds)
     {
-        return __builtin_bit_cast(bf16x8_t, *(lds_uint4_t*)(uintptr_t)lds);
+        return __builtin_bit_cast(bf16x8_t, *(const lds_chunk_t*)(uintptr_t)lds);
     }
 
     static __device__ __forceinline__ void run(const AttnArgs& a, const Item& it, char* smem)
@@ -240,11 +247,17 @@ template <bool FP8, int DP> struct Many {
             }
         }
         const bool idle = rg.first + wave * 32 >= rg.rows;           // a wave whose rows are none stages all the same
+        // The compiler counts the loads it knows: without this wait it would put one for the queries into the loop, where it would
+        // also wait for the loads of the step after.
+        __builtin_amdgcn_s_waitcnt(0x0f70);                          // vmcnt(0)
         int at = 0;                                                  // byte offset of the step's stage
         while (cur.t < rg.end) {
             if constexpr (FP8) wait_lds_reads();
             else wait_vmcnt<0>();
             block_barrier();
+            // a step whose tokens not every row sees
+            const bool masked = cur.t + TOK > rg.full_hi || cur.t < rg.full_lo || cur.there != 0xffu;
+            if (masked) clean_values(cur, rg, me, v_at, lds0 + at + HALF, smem, o);
             Step next{cur.t + TOK, 0};
             const bool more = next.t < rg.end;
             if (more) {
@@ -255,13 +268,11 @@ template <bool FP8, int DP> struct Many {
             if (!idle) {
                 float16_t s[2];
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    s[b] = float16_t{};
+                for (int c = 0; c < DP / 16; ++c)
 #pragma unroll
-                    for (int c = 0; c < DP / 16; ++c)
-                        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_keys(k_at[c] + b * 32 * ROWB), qf[c], s[b], 0, 0, 0);
-                }
-                const bool masked = cur.t + TOK > rg.full_hi || cur.t < rg.full_lo || cur.there != 0xffu;
+                    for (int b = 0; b < 2; ++b)
+                        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_keys(k_at[c] + b * 32 * ROWB), qf[c], c == 0 ? float16_t{} : s[b],
+                                                                       0, 0, 0);
                 if (masked) {
 #pragma unroll
                     for (int b = 0; b < 2; ++b)
@@ -300,18 +311,11 @@ template <bool FP8, int DP> struct Many {
                     }
                     w[k] = __builtin_bit_cast(bf16x8_t, make_uint4(u[0], u[1], u[2], u[3]));
                 }
-                if (!masked) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
+                for (int k = 0; k < 4; ++k)
 #pragma unroll
-                        for (int x = 0; x < NB; ++x) {
-                            const uint2 lo = read_transposed(v_at[0][x] + k * 16 * ROWB), hi = read_transposed(v_at[1][x] + k * 16 * ROWB);
-                            o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                                __builtin_bit_cast(bf16x8_t, make_uint4(lo.x, lo.y, hi.x, hi.y)), w[k], o[x], 0, 0, 0);
-                        }
-                } else {
-                    careful_values(cur, rg, me, v_at, w, o);
-                }
+                    for (int x = 0; x < NB; ++x)
+                        o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_values(v_at, k, x), w[k], o[x], 0, 0, 0);
             }
             if constexpr (FP8)
                 if (more) widen(smem + (at ^ STAGE));
@@ -355,62 +359,80 @@ template <bool FP8, int DP> struct Many {
         }
     }
 
-    // The second product for a step whose tokens not every row sees: values of tokens that are not there, or that no row sees, are
-    // zeros whatever the cache holds, and those that are not finite (a weight of zero would not keep them out) go to the rows
-    // that see them as the infinity or NaN that they are.
-    static __device__ __forceinline__ void careful_values(const Step& cur, const Range& rg, const Row& me, const uint32_t (&v_at)[2][NB],
-                                                          const bf16x8_t (&w)[4], float16_t (&o)[NB])
+    // The values of a step whose tokens not every row sees, made fit for the second product, where a weight of zero keeps only finite
+    // values out: tokens that are not there, or that no row sees, become zeros, whatever the cache holds; where there is an infinity or NaN
+    // among the others, the rows that see it get it right away, and it becomes a zero too.  Every thread of the block calls it.
+    static __device__ __forceinline__ void clean_values(const Step& cur, const Range& rg, const Row& me, const uint32_t (&v_at)[2][NB],
+                                                        uint32_t values, char* smem, float16_t (&o)[NB])
+    {
+        int32_t* flag = reinterpret_cast<int32_t*>(smem + 2 * STAGE);
+        auto mine = [&](auto f) {
+            for (int i = threadIdx.x; i < TOK * CH; i += 256) {
+                const int tl = i / CH;
+                uint4 v = read_chunk(values + i * 16);
+                if (f(v, ((cur.there >> (tl / 8)) & 1) != 0 && cur.t + tl < rg.hi)) write_chunk(values + i * 16, v);
+            }
+        };
+        if (threadIdx.x == 0) *flag = 0;
+        __syncthreads();
+        mine([&](uint4& v, bool there) {
+            if (!there) {
+                v = make_uint4(0, 0, 0, 0);
+                return true;
+            }
+            if (strange(v.x) | strange(v.y) | strange(v.z) | strange(v.w)) *flag = 1;
+            return false;
+        });
+        __syncthreads();
+        if (*flag == 0) return;
+        give_strange_values(cur, me, v_at, o);
+        __syncthreads();
+        mine([&](uint4& v, bool) {
+            v.x = finite_of(v.x); v.y = finite_of(v.y); v.z = finite_of(v.z); v.w = finite_of(v.w);
+            return true;
+        });
+        __syncthreads();
+    }
+    static __device__ __forceinline__ void give_strange_values(const Step& cur, const Row& me, const uint32_t (&v_at)[2][NB], float16_t (&o)[NB])
     {
         const int h = lane_id() >> 5;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            uint32_t keep[4], seen[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                keep[i] = seen[i] = 0;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int grp = 2 * k + i / 2, tok = cur.t + grp * 8 + 4 * h + (i % 2) * 2 + e;
-                    const bool there = (cur.there >> grp) & 1;
-                    if (there && tok < rg.hi) keep[i] |= 0xffffu << (16 * e);
-                    if (there && tok < me.see_hi && tok >= me.see_lo) seen[i] |= 0x3f80u << (16 * e);
-                }
-            }
-#pragma unroll
-            for (int x = 0; x < NB; ++x) {
-                const uint2 lo = read_transposed(v_at[0][x] + k * 16 * ROWB), hi = read_transposed(v_at[1][x] + k * 16 * ROWB);
-                uint32_t v[4] = {lo.x & keep[0], lo.y & keep[1], hi.x & keep[2], hi.y & keep[3]};
-                bool strange = false;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) strange |= (v[i] & 0x7f80u) == 0x7f80u || (v[i] & 0x7f800000u) == 0x7f800000u;
-                if (__any(strange)) {
+        for (int x = 0; x < NB; ++x)
 #pragma unroll 1
-                    for (int what = 1; what <= 3; ++what) {          // infinity, minus infinity, NaN
-                        uint32_t mark[4];
+            for (int k = 0; k < 4; ++k) {
+                uint32_t seen[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            mark[i] = 0;
+                for (int i = 0; i < 4; ++i) {
+                    seen[i] = 0;
 #pragma unroll
-                            for (int e = 0; e < 2; ++e)
-                                if (kind((v[i] >> (16 * e)) & 0xffffu) == what) mark[i] |= 0x3f80u << (16 * e);
-                        }
-                        const float16_t hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            __builtin_bit_cast(bf16x8_t, make_uint4(mark[0], mark[1], mark[2], mark[3])),
-                            __builtin_bit_cast(bf16x8_t, make_uint4(seen[0], seen[1], seen[2], seen[3])), float16_t{}, 0, 0, 0);
-                        const float worth = what == 1 ? __builtin_inff() : what == 2 ? -__builtin_inff() : __builtin_nanf("");
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) o[x][r] += hits[r] > 0.5f ? worth : 0.0f;
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (kind(v[i] & 0xffffu) != 0) v[i] &= 0xffff0000u;
-                        if (kind(v[i] >> 16) != 0) v[i] &= 0xffffu;
+                    for (int e = 0; e < 2; ++e) {
+                        const int grp = 2 * k + i / 2, tok = cur.t + grp * 8 + 4 * h + (i % 2) * 2 + e;
+                        if (((cur.there >> grp) & 1) && tok < me.see_hi && tok >= me.see_lo) seen[i] |= 0x3f80u << (16 * e);
                     }
                 }
-                o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, make_uint4(v[0], v[1], v[2], v[3])), w[k], o[x],
-                                                               0, 0, 0);
+                const uint4 v = __builtin_bit_cast(uint4, read_values(v_at, k, x));
+                const uint32_t vv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll 1
+                for (int what = 1; what <= 3; ++what) {
+                    uint32_t mark[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        mark[i] = (kind(vv[i] & 0xffffu) == what ? 0x3f80u : 0u) | (kind(vv[i] >> 16) == what ? 0x3f800000u : 0u);
+                    const float16_t hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        __builtin_bit_cast(bf16x8_t, make_uint4(mark[0], mark[1], mark[2], mark[3])),
+                        __builtin_bit_cast(bf16x8_t, make_uint4(seen[0], seen[1], seen[2], seen[3])), float16_t{}, 0, 0, 0);
+                    const float worth = what == 1 ? __builtin_inff() : what == 2 ? -__builtin_inff() : __builtin_nanf("");
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[x][r] += hits[r] > 0.5f ? worth : 0.0f;
+                }
             }
-        }
+    }
+    static __device__ __forceinline__ uint4 read_chunk(uint32_t lds) { return __builtin_bit_cast(uint4, *(const lds_chunk_t*)(uintptr_t)lds); }
+    static __device__ __forceinline__ void write_chunk(uint32_t lds, uint4 v) { *(lds_chunk_t*)(uintptr_t)lds = __builtin_bit_cast(uint32x4_t, v); }
+    static __device__ __forceinline__ bool strange(uint32_t v) { return ((v & 0x7f80u) == 0x7f80u) | ((v & 0x7f800000u) == 0x7f800000u); }
+    static __device__ __forceinline__ uint32_t finite_of(uint32_t v)
+    {
+        return (kind(v & 0xffffu) == 0 ? v & 0xffffu : 0u) | (kind(v >> 16) == 0 ? v & 0xffff0000u : 0u);
     }
     // 0 finite, 1 infinity, 2 minus infinity, 3 NaN
     static __device__ __forceinline__ int kind(uint32_t u) { return (u & 0x7f80u) != 0x7f80u ? 0 : (u & 0x7fu) ? 3 : (u >> 15) ? 2 : 1; }
