@@ -18,14 +18,14 @@ template <typename T, bool FP8, int DP> constexpr size_t lds_bytes()
 {
     const size_t few = sizeof(typename Few<T, FP8, DP, few_rows<T, FP8, DP>() / 16>::Shared);
     const size_t many = sizeof(T) == 2 ? Many<FP8, DP>::LDS : 0;
-    return few > many ? few : many;
+    return ((few > many ? few : many) + 15) / 16 * 16;
 }
 
 template <typename T, bool FP8, int DP> __global__ __launch_bounds__(256, sizeof(T) == 4 || DP > 128 ? 1 : 2) void attention_kernel(AttnArgs a)
 {
     extern __shared__ __attribute__((aligned(256))) char smem[];
     constexpr int NQ = few_rows<T, FP8, DP>() / 16;
-    const Item it = find_item(a, blockIdx.x);
+    const Item it = find_item(a, blockIdx.x, *reinterpret_cast<PlanShared*>(smem + lds_bytes<T, FP8, DP>()));
     if (!it.valid) return;
     if (it.q.many) {
         if constexpr (sizeof(T) == 2) Many<FP8, DP>::run(a, it, smem);
@@ -40,6 +40,8 @@ template <typename T, bool FP8, int DP> hipError_t launch(AttnArgs a, hipStream_
 {
     a.few_rows = few_rows<T, FP8, DP>();
     a.tile_rows = sizeof(T) == 2 ? kManyRows : a.few_rows;
+    a.tile_tokens = a.tile_rows / a.G;
+    a.g_magic = map_magic_of(a.G);
     // a block for every item there can be: a tile for a sequence and for tile_rows more packed rows; pieces are kFewItems and kTileItems
     // more at most (and a few for the rounding of their lengths), fewer where no history is long
     const int64_t tiles = (int64_t)(a.c.S < a.c.T ? a.c.S : a.c.T) + (int64_t)a.c.T * a.G / a.tile_rows;
@@ -47,9 +49,9 @@ template <typename T, bool FP8, int DP> hipError_t launch(AttnArgs a, hipStream_
     const int64_t longest = (int64_t)a.c.max_pages << a.c.page_shift;
     const int64_t by_length = longest > kMinPiece ? base * ((longest - 1) / kMinPiece) : 0;
     const int64_t most = kFewItems + kTileItems + 64;
-    const int64_t grid = base + (by_length < most ? by_length : most);
+    const int64_t grid = base + (by_length < most ? by_length : most) + 16;      // (either kind's items are dealt out by eights)
     if (grid > 0x7fffffff) return hipErrorInvalidValue;
-    constexpr size_t lds = lds_bytes<T, FP8, DP>();
+    constexpr size_t lds = lds_bytes<T, FP8, DP>() + sizeof(PlanShared);
     static bool done[kMaxDevices];
     const auto kern = attention_kernel<T, FP8, DP>;
     const hipError_t e = ensure_lds_limit(kern, lds, done);

@@ -15,9 +15,9 @@ typedef float float16_t __attribute__((ext_vector_type(16)));
 constexpr float kLowest = -FLT_MAX;      // a running maximum before its first token: finite, so that no difference is NaN
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
-// Items that the pieces of a launch aim at, of each kind of tile.  Pieces are no shorter than kMinPiece tokens (a step of 32 for each
-// of a block's four waves) or kMinTilePiece.
-constexpr int kFewItems = 2048, kTileItems = 512;
+// Items that the pieces of a launch aim at, of each kind of tile.  Pieces are multiples of kMinPiece tokens (a step of 32 for each of
+// a block's four waves), and no shorter than kMinTilePiece where a tile has many rows.
+constexpr int kFewItems = 1024, kTileItems = 512;
 constexpr int kMinPiece = 128, kMinTilePiece = 256;
 
 struct Seq {
@@ -36,22 +36,20 @@ struct Item {
 __device__ __forceinline__ Seq shape_of(const AttnArgs& a, int lo, int hi, int kv)
 {
     Seq q;
-    lo = lo < 0 ? 0 : (lo > a.c.T ? a.c.T : lo);
-    hi = hi < lo ? lo : (hi > a.c.T ? a.c.T : hi);
     const int most = a.c.max_pages << a.c.page_shift;
     q.row0 = lo;
     q.n = hi - lo;
     q.kv = kv < 0 ? 0 : (kv > most ? most : kv);
     const int rows = q.n * a.G;
     q.many = rows > a.few_rows && a.tile_rows > a.few_rows;
-    const int per = rows <= 16 ? 16 : rows <= a.few_rows ? a.few_rows : a.tile_rows;
+    const int per = rows <= 16 ? 16 : rows <= a.few_rows ? a.few_rows : a.tile_rows;      // (all powers of two)
     q.units = per / 16;
-    q.tiles = (rows + per - 1) / per;
+    q.tiles = (rows + per - 1) >> (31 - __builtin_clz(per));
     q.len = q.kv;
     if (a.window > 0) {
         const int first = q.kv - q.n - a.window + 1;
         int len = q.kv - (first > 0 ? first : 0) + 31;
-        const int one = a.window + per / a.G + 2 + 31;       // (windows are at most 2^30)
+        const int one = a.window + a.tile_tokens + 2 + 31;   // (windows are at most 2^30)
         if (a.causal && one < len) len = one;
         if (len < q.len) q.len = len;
     }
@@ -61,148 +59,160 @@ __device__ __forceinline__ Seq shape_of(const AttnArgs& a, int lo, int hi, int k
 __device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
 __device__ __forceinline__ float last_lane(float v) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63)); }
 
-// The largest of `first` and the values of the lanes below.
-__device__ __forceinline__ int wave_max_below(int v, int first)
-{
-    int x = __builtin_amdgcn_update_dpp(first, v, 0x138, 0xF, 0xF, false);      // the lane below's; lane 0: first
-    auto step = [&](auto ctrl, auto row_mask) {
-        const int o = __builtin_amdgcn_update_dpp(x, x, decltype(ctrl)::value, decltype(row_mask)::value, 0xF, false);
-        x = o > x ? o : x;
-    };
-    using std::integral_constant;
-    step(integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{});
-    step(integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{});
-    step(integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});
-    step(integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});
-    step(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});
-    step(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});
-    return x;
-}
+struct PlanShared {
+    float work[2][4];
+    int sums[3][4], bad[4];
+    int found[10];
+};
 
-// The item of block `block`.  Sequences are taken 256 at a time, four to a lane.  Tiles of many rows come first: they take longest.
-// A sequence whose partial results no longer fit the workspace stays in one piece.
-__device__ __forceinline__ Item find_item(const AttnArgs& a, int block)
+// The item of a block, the same in all of its threads.  A thread takes a sequence (256 at a time), so that the code is short: every
+// block of a launch runs it before it can load anything, and code that runs once costs its instruction misses.
+// Offsets that descend, or leave [0, T], would name rows twice or none: then there are no items at all.
+__device__ __forceinline__ Item find_item(const AttnArgs& a, int block, PlanShared& sh)
 {
-    const int lane = lane_id();
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int S = a.c.S, Hk = a.c.Hk;
-    Seq q[4];
-    int start = 0;                  // where the sequences before a load's end
+    Seq q;
+    bool bad = false;
     auto load = [&](int b) {
-        if (b == 0) start = 0;
-        int off[5], kv[4];
-#pragma unroll
-        for (int i = 0; i < 5; ++i) {
-            const int s = b + lane * 4 + i;
-            off[i] = a.c.off[s < S ? s : S];
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int s = b + lane * 4 + i;
-            kv[i] = a.c.lens[s < S ? s : S - 1];
-        }
-        // Offsets that descend would name rows twice; a sequence starts no earlier than all before it have ended, so there are never more
-        // rows than T, nor more items than the launch has blocks.
-#pragma unroll
-        for (int i = 0; i < 4; ++i) off[i + 1] = off[i + 1] > off[i] ? off[i + 1] : off[i];
-        int before = wave_max_below(off[4], start);
-        start = last_lane(before > off[4] ? before : off[4]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int lo = before > off[i] ? before : off[i], hi = b + lane * 4 + i < S ? (before > off[i + 1] ? before : off[i + 1]) : lo;
-            q[i] = shape_of(a, lo, hi, kv[i]);
-        }
+        const int s = b + (int)threadIdx.x;
+        const int lo = a.c.off[s < S ? s : S], hi = a.c.off[s < S ? s + 1 : S], kv = a.c.lens[s < S ? s : S - 1];
+        bad |= (lo < 0) | (hi < lo) | (hi > a.c.T);
+        q = shape_of(a, lo, bad ? lo : hi, kv);
     };
+    // the batch's work in tokens of a tile, of few rows and of many
     float few = 0, many = 0;
     for (int b = 0; b < S; b += 256) {
         load(b);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float w = (float)q[i].tiles * (float)q[i].len;
-            (q[i].many ? many : few) += w;
-        }
+        const float w = (float)q.tiles * (float)q.len;
+        (q.many ? many : few) += w;
     }
-    few = last_lane(wave_scan(few)) * (float)Hk;
-    many = last_lane(wave_scan(many)) * (float)Hk;
+    few = wave_scan(few);
+    many = wave_scan(many);
+    if (lane == 63) {
+        sh.work[0][wave] = few;
+        sh.work[1][wave] = many;
+    }
+    const bool any_bad = __any(bad);
+    if (lane == 0) sh.bad[wave] = any_bad;
+    __syncthreads();
+    Item it;
+    it.valid = false;
+    if (sh.bad[0] | sh.bad[1] | sh.bad[2] | sh.bad[3]) return it;
+    few = (sh.work[0][0] + sh.work[0][1] + sh.work[0][2] + sh.work[0][3]) * (float)Hk;
+    many = (sh.work[1][0] + sh.work[1][1] + sh.work[1][2] + sh.work[1][3]) * (float)Hk;
     // A token costs an item of either kind about the same time (of a unit's share of the memory, or of its matrix cores).
     auto even = [](float work, int items, int least) {
         const float v = work * (1.0f / (float)items);
         return v <= (float)least ? least : v < 1e9f ? ((int)v + least) / least * least : 1 << 30;
     };
-    const int few_piece = even(few, kFewItems, kMinPiece), many_piece = even(few + many, kTileItems, kMinTilePiece);
+    int few_piece = even(few, kFewItems, kMinPiece), many_piece = even(few + many, kTileItems, kMinTilePiece);
 
-    Item it;
-    it.valid = false;
-    int items0 = 0;
-    for (int pass = many > 0 ? 0 : 1; pass < 2; ++pass) {
-        float slots0 = 0;           // (as floats: they only grow, and past the workspace only that counts)
+    // items of many rows and of few, and units of partial results, of this thread's sequence
+    int count[2], need, pieces;
+    auto count_items = [&]() {
+        const int piece = q.many ? many_piece : few_piece;
+        pieces = q.len > piece ? (q.len + piece - 1) / piece : 1;
+        const int n = q.tiles * Hk * pieces;
+        count[0] = q.many ? n : 0;
+        count[1] = q.many ? 0 : n;
+        need = pieces > 1 ? n * q.units : 0;
+    };
+    int total[3] = {0, 0, 0}, incl[3], below[3];
+    // inclusive sums over the block's threads so far: incl (of the wave) + below (of the waves before)
+    auto scan = [&](int c0, int c1, int c2) {
+        incl[0] = wave_scan(c0);
+        incl[1] = wave_scan(c1);
+        incl[2] = wave_scan(c2);
+        __syncthreads();
+        if (lane == 63) {
+#pragma unroll
+            for (int k = 0; k < 3; ++k) sh.sums[k][wave] = incl[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            below[k] = 0;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int v = sh.sums[k][w];
+                below[k] += w < wave ? v : 0;
+                total[k] += v;
+            }
+        }
+    };
+    for (;;) {
+        int c0 = 0, c1 = 0, c2 = 0;
         for (int b = 0; b < S; b += 256) {
             if (S > 256) load(b);
-            int pieces[4];
-            float need[4], want = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int piece = q[i].many ? many_piece : few_piece;
-                pieces[i] = q[i].len > piece ? (q[i].len + piece - 1) / piece : 1;
-                need[i] = pieces[i] > 1 ? (float)(q[i].tiles * q[i].units) * (float)(Hk * pieces[i]) : 0.0f;
-                want += need[i];
-            }
-            const float incl = wave_scan(want);
-            float at = slots0 + incl - want;
-            int mine = 0, slot[4], count[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                slot[i] = 0;
-                if (need[i] > 0) {
-                    if (at + need[i] <= (float)kPartUnits) slot[i] = (int)at;
-                    else pieces[i] = 1;
-                }
-                at += need[i];
-                count[i] = q[i].many == (pass == 0) ? q[i].tiles * Hk * pieces[i] : 0;
-                mine += count[i];
-            }
-            slots0 += last_lane(incl);
-            const int incl_items = items0 + wave_scan(mine);
-            const unsigned long long hit = __ballot(block < incl_items);
-            if (hit != 0) {
-                const int src = __ffsll((long long)hit) - 1;
-                int rem = block - (incl_items - mine);
-                int seq = 0, sl = 0, pc = 1;
-                Seq f = q[0];
-                bool found = false;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (!found && rem < count[i]) {
-                        found = true;
-                        f = q[i];
-                        seq = b + lane * 4 + i;
-                        sl = slot[i];
-                        pc = pieces[i];
-                    } else if (!found) {
-                        rem -= count[i];
-                    }
-                }
-                auto pick = [&](int v) { return __builtin_amdgcn_readlane(v, src); };
-                it.q.row0 = pick(f.row0); it.q.n = pick(f.n); it.q.kv = pick(f.kv);
-                it.q.tiles = pick(f.tiles); it.q.units = pick(f.units); it.q.len = pick(f.len);
-                it.q.many = pass == 0;
-                it.seq = pick(seq);
-                rem = pick(rem);
-                sl = pick(sl);
-                pc = pick(pc);
-                // heads side by side (they go to different XCDs, and the tiles of a head to the same ones), long tiles first
-                it.head = rem % Hk;
-                rem /= Hk;
-                it.sub = rem % pc;
-                it.tile = it.q.tiles - 1 - rem / pc;
-                it.piece = pc == 1 ? 0 : it.q.many ? many_piece : few_piece;
-                it.slot = sl + (it.tile * Hk + it.head) * pc * it.q.units;
-                it.valid = rem >= 0 && it.tile >= 0;      // (always, but for descriptors so wrong that the counts overflow)
-                return it;
-            }
-            items0 = last_lane(incl_items);
+            count_items();
+            c0 += count[0];
+            c1 += count[1];
+            c2 += need;
         }
+        total[0] = total[1] = total[2] = 0;
+        scan(c0, c1, c2);
+        if (total[2] <= kPartUnits) break;
+        few_piece = many_piece = 1 << 30;      // (more pieces than the workspace holds: none are split)
     }
+    // Of a batch with both kinds of tile, eight blocks take items of many rows and eight of few, in turn and as often as keeps pace with
+    // their numbers: a unit then streams a cache for one block while another one keeps its matrix cores busy.  (Eight at a
+    // time, so that an item's number still decides its XCD.)
+    int kind = total[0] > 0 ? 0 : 1;
+    if (total[0] > 0 && total[1] > 0) {
+        const int groups = (total[0] + 7) / 8, fews = (total[1] + 7) / 8;
+        // of the first g groups of blocks, this many are of many rows
+        const float part = (float)groups / (float)(groups + fews);
+        auto of_many = [&](int g) {
+            const int n = (int)__builtin_ceilf((float)g * part);
+            return n < groups ? n : groups;
+        };
+        const int g = block / 8, before = g < groups + fews ? of_many(g) : groups, until = g + 1 < groups + fews ? of_many(g + 1) : groups;
+        kind = until > before ? 0 : 1;
+        block = (kind == 0 ? before : g - before) * 8 + block % 8;
+    }
+    if (block >= total[kind]) return it;
+    if (S > 256) total[0] = total[1] = total[2] = 0;
+    for (int b = 0; b < S; b += 256) {
+        int before = 0, slots = 0;
+        if (S > 256) {
+            before = total[kind];
+            slots = total[2];
+            load(b);
+            count_items();
+            scan(count[0], count[1], need);
+        }
+        const int n = count[kind], rem = block - (before + below[kind] + incl[kind] - n);
+        if (rem >= 0 && rem < n) {
+            sh.found[0] = q.row0; sh.found[1] = q.n; sh.found[2] = q.kv; sh.found[3] = q.tiles; sh.found[4] = q.units;
+            sh.found[5] = b + threadIdx.x; sh.found[6] = rem; sh.found[7] = pieces; sh.found[8] = slots + below[2] + incl[2] - need;
+        }
+        if (S > 256 && block < total[kind]) break;
+    }
+    __syncthreads();
+    auto get = [&](int i) { return __builtin_amdgcn_readfirstlane(sh.found[i]); };
+    it.q.row0 = get(0); it.q.n = get(1); it.q.kv = get(2); it.q.tiles = get(3); it.q.units = get(4);
+    it.q.many = kind == 0;
+    it.seq = get(5);
+    int rem = get(6);
+    const int pc = get(7);
+    // heads side by side (they go to different XCDs, and the tiles of a head to the same ones), long tiles first
+    it.head = rem % Hk;
+    rem /= Hk;
+    it.sub = rem % pc;
+    it.tile = it.q.tiles - 1 - rem / pc;
+    it.piece = pc == 1 ? 0 : it.q.many ? many_piece : few_piece;
+    it.slot = get(8) + (it.tile * Hk + it.head) * pc * it.q.units;
+    it.valid = true;
     return it;
+}
+
+// The new token of packed row r: r / G, from ceil(2^32 / G) (one too high at most).
+__device__ __forceinline__ int token_of(const AttnArgs& a, int r)
+{
+    if (a.G == 1) return r;
+    const uint32_t q = __umulhi((uint32_t)r, a.g_magic);
+    return (int)(q * (uint32_t)a.G > (uint32_t)r ? q - 1 : q);
 }
 
 // The tokens that a tile's rows see: all rows those of [full_lo, full_hi), some row those of [lo, hi); lo is a multiple of 32.
@@ -221,7 +231,7 @@ __device__ __forceinline__ Range range_of(const AttnArgs& a, const Item& it)
     const int end = r.first + it.q.units * 16;
     const int last = (end < r.rows ? end : r.rows) - 1;
     r.p0 = it.q.kv - it.q.n;
-    const int p_first = r.p0 + r.first / a.G, p_last = r.p0 + last / a.G;
+    const int p_first = r.p0 + token_of(a, r.first), p_last = r.p0 + token_of(a, last);
     r.hi = a.causal && p_last + 1 < it.q.kv ? p_last + 1 : it.q.kv;
     if (r.hi < 0) r.hi = 0;
     r.full_hi = a.causal && p_first + 1 < it.q.kv ? p_first + 1 : it.q.kv;
@@ -233,8 +243,11 @@ __device__ __forceinline__ Range range_of(const AttnArgs& a, const Item& it)
     r.begin = r.lo;
     r.end = r.hi;
     if (r.pieces > 1) {
-        r.begin += it.sub * it.piece;
-        if (r.end - r.begin > it.piece) r.end = r.begin + it.piece;
+        // (nearly) equal pieces, whole steps of every kernel
+        const int steps = (len + kMinPiece - 1) / kMinPiece, each = steps / r.pieces, extra = steps - each * r.pieces;
+        r.begin += (it.sub * each + (it.sub < extra ? it.sub : extra)) * kMinPiece;
+        const int end = r.begin + (each + (it.sub < extra ? 1 : 0)) * kMinPiece;
+        if (end < r.end) r.end = end;
     }
     return r;
 }
@@ -249,7 +262,7 @@ __device__ __forceinline__ Row row_of(const AttnArgs& a, const Item& it, const R
 {
     Row x;
     x.there = r < rg.rows;
-    const int tok = x.there ? r / a.G : 0;
+    const int tok = x.there ? token_of(a, r) : 0;
     x.row = it.q.row0 + tok;
     x.head = it.head * a.G + (x.there ? r - tok * a.G : 0);
     const int p = rg.p0 + tok;
