@@ -13,33 +13,43 @@
 namespace moe {
 namespace {
 
-template <typename T, bool FP8, int DP> constexpr int few_rows() { return DP <= 128 ? 32 : 16; }      // 32 rows of 256 dimensions do not fit the registers
-template <typename T, bool FP8, int DP> constexpr size_t lds_bytes()
-{
-    const size_t few = sizeof(typename Few<T, FP8, DP, few_rows<T, FP8, DP>() / 16>::Shared);
-    const size_t many = sizeof(T) == 2 ? Many<FP8, DP>::LDS : 0;
-    return ((few > many ? few : many) + 15) / 16 * 16;
-}
+// The kernel of a batch.  LIGHT: every tile has 16 rows, which needs fewer registers, so that more blocks share a unit.
+template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> struct Kernel {
+    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr int NQ = LIGHT || DP > 128 ? 1 : 2;      // (32 rows of 256 dimensions do not fit the registers)
+    static constexpr bool MANY = !F32 && !LIGHT;
+    static constexpr int BLOCKS = LIGHT ? (F32 ? (DP > 128 ? 1 : 2) : DP > 128 ? (FP8 ? 2 : 1) : DP > 64 ? (FP8 || EXACT ? 3 : 2) : 4) : (F32 || DP > 128 ? 1 : 2);      // of a unit
+    static constexpr size_t PLAN_AT = ((MANY && Many<FP8, DP, EXACT>::LDS > sizeof(typename Few<T, FP8, DP, NQ, EXACT>::Shared) ? Many<FP8, DP, EXACT>::LDS
+                                                                                                             : sizeof(typename Few<T, FP8, DP, NQ, EXACT>::Shared)) + 15) / 16 * 16;
+    static constexpr size_t LDS = PLAN_AT + sizeof(PlanShared);
+};
 
-template <typename T, bool FP8, int DP> __global__ __launch_bounds__(256, sizeof(T) == 4 || DP > 128 ? 1 : 2) void attention_kernel(AttnArgs a)
+template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> __global__ __launch_bounds__(256, (Kernel<T, FP8, DP, EXACT, LIGHT>::BLOCKS)) void attention_kernel(AttnArgs a)
 {
+    typedef Kernel<T, FP8, DP, EXACT, LIGHT> K;
     extern __shared__ __attribute__((aligned(256))) char smem[];
-    constexpr int NQ = few_rows<T, FP8, DP>() / 16;
-    const Item it = find_item(a, blockIdx.x, *reinterpret_cast<PlanShared*>(smem + lds_bytes<T, FP8, DP>()));
+    const Item it = find_item(a, blockIdx.x, *reinterpret_cast<PlanShared*>(smem + K::PLAN_AT));
     if (!it.valid) return;
-    if (it.q.many) {
-        if constexpr (sizeof(T) == 2) Many<FP8, DP>::run(a, it, smem);
-    } else if (it.q.units == 1) {
-        Few<T, FP8, DP, 1>::run(a, it, *reinterpret_cast<typename Few<T, FP8, DP, 1>::Shared*>(smem));
-    } else if constexpr (NQ > 1) {
-        Few<T, FP8, DP, NQ>::run(a, it, *reinterpret_cast<typename Few<T, FP8, DP, NQ>::Shared*>(smem));
+    if constexpr (K::MANY) {
+        if (it.q.many) {
+            Many<FP8, DP, EXACT>::run(a, it, smem);
+            return;
+        }
     }
+    if constexpr (K::NQ > 1) {
+        if (it.q.units > 1) {
+            Few<T, FP8, DP, K::NQ, EXACT>::run(a, it, *reinterpret_cast<typename Few<T, FP8, DP, K::NQ, EXACT>::Shared*>(smem));
+            return;
+        }
+    }
+    Few<T, FP8, DP, 1, EXACT>::run(a, it, *reinterpret_cast<typename Few<T, FP8, DP, 1, EXACT>::Shared*>(smem));
 }
 
-template <typename T, bool FP8, int DP> hipError_t launch(AttnArgs a, hipStream_t s)
+template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> hipError_t launch(AttnArgs a, hipStream_t s)
 {
-    a.few_rows = few_rows<T, FP8, DP>();
-    a.tile_rows = sizeof(T) == 2 ? kManyRows : a.few_rows;
+    typedef Kernel<T, FP8, DP, EXACT, LIGHT> K;
+    a.few_rows = K::NQ * 16;
+    a.tile_rows = K::MANY ? kManyRows : a.few_rows;
     a.tile_tokens = a.tile_rows / a.G;
     a.g_magic = map_magic_of(a.G);
     // a block for every item there can be: a tile for a sequence and for tile_rows more packed rows; pieces are kFewItems and kTileItems
@@ -51,20 +61,30 @@ template <typename T, bool FP8, int DP> hipError_t launch(AttnArgs a, hipStream_
     const int64_t most = kFewItems + kTileItems + 64;
     const int64_t grid = base + (by_length < most ? by_length : most) + 16;      // (either kind's items are dealt out by eights)
     if (grid > 0x7fffffff) return hipErrorInvalidValue;
-    constexpr size_t lds = lds_bytes<T, FP8, DP>() + sizeof(PlanShared);
     static bool done[kMaxDevices];
-    const auto kern = attention_kernel<T, FP8, DP>;
-    const hipError_t e = ensure_lds_limit(kern, lds, done);
+    const auto kern = attention_kernel<T, FP8, DP, EXACT, LIGHT>;
+    const hipError_t e = ensure_lds_limit(kern, K::LDS, done);
     if (e != hipSuccess) return e;
-    kern<<<(unsigned)grid, 256, lds, s>>>(a);
+    kern<<<(unsigned)grid, 256, K::LDS, s>>>(a);
     return hipGetLastError();
+}
+
+template <typename T, bool FP8, int DP> hipError_t launch_by_rows(const AttnArgs& a, hipStream_t s)
+{
+    // How rows spread over the sequences only the device knows; with no more than 16 packed rows to a sequence on average, a batch is
+    // taken for one of decode rows.  (Right for any spread: a sequence with more rows has more tiles.)
+    const bool light = (int64_t)a.c.T * a.G <= (int64_t)16 * a.c.S;
+    if constexpr (sizeof(T) == 2) {
+        if (a.c.D == DP) return light ? launch<T, FP8, DP, true, true>(a, s) : launch<T, FP8, DP, true, false>(a, s);
+    }
+    return light ? launch<T, FP8, DP, false, true>(a, s) : launch<T, FP8, DP, false, false>(a, s);
 }
 
 template <typename T, bool FP8> hipError_t launch_by_dim(const AttnArgs& a, hipStream_t s)
 {
-    if (a.c.D <= 64) return launch<T, FP8, 64>(a, s);
-    if (a.c.D <= 128) return launch<T, FP8, 128>(a, s);
-    return launch<T, FP8, 256>(a, s);
+    if (a.c.D <= 64) return launch_by_rows<T, FP8, 64>(a, s);
+    if (a.c.D <= 128) return launch_by_rows<T, FP8, 128>(a, s);
+    return launch_by_rows<T, FP8, 256>(a, s);
 }
 
 }  // namespace

@@ -31,7 +31,8 @@ __device__ __forceinline__ float sum_over_tokens(float v)
 // eight tokens' dwords are put together by byte permutes, which is all the transposing there is.
 // The four waves of a block take a quarter of the piece each and join through LDS.
 // ----------------------------------------------------------------------------------------------------------------
-template <typename T, bool FP8, int DP, int NQ> struct Few {
+// EXACT: the heads are DP wide, no less, and every offset within a row is a constant.
+template <typename T, bool FP8, int DP, int NQ, bool EXACT> struct Few {
     static constexpr bool F32 = sizeof(T) == 4;
     static constexpr int NJ = F32 ? 1 : 2, TOK = NJ * 16;          // 16-token subtiles of a step
     static constexpr int ESZ = FP8 ? 1 : (int)sizeof(T);
@@ -59,11 +60,15 @@ template <typename T, bool FP8, int DP, int NQ> struct Few {
         if (it.sub >= rg.pieces) return;
         const int lane = lane_id(), n = lane & 15, g = lane >> 4;
         const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-        const int D = a.c.D, shift = a.c.page_shift, Hk = a.c.Hk;
+        const int D = EXACT ? DP : a.c.D, shift = a.c.page_shift, Hk = a.c.Hk;
         const int begin = rg.begin, end = rg.end;
         const int per = end > begin ? (end - begin + 4 * TOK - 1) / (4 * TOK) * TOK : 0;
         const int t0 = begin + wave * per;
         const int t1 = t0 + per < end ? t0 + per : end;
+
+        // the page table first: everything waits for it
+        Entries pages;
+        if (t0 < t1) pages.hold(a.c, it.seq, t0 >> shift, t1);
 
         // rows: what each sees, and its queries
         int see_lo[NQ], see_hi[NQ];
@@ -105,7 +110,6 @@ template <typename T, bool FP8, int DP, int NQ> struct Few {
             for (int f = 0; f < VW; ++f) o[f / PER][i][f % PER] = float4_t{0, 0, 0, 0};
         }
 
-        Entries pages;
         auto page_of = [&](int t) { return __shfl(pages.id, (t >> shift) - pages.base); };
         auto slot_of = [&](int id, int t) {
             return page_row(id < 0 ? 0 : id, Hk, it.head, shift, t & ((1 << shift) - 1));
@@ -149,7 +153,6 @@ template <typename T, bool FP8, int DP, int NQ> struct Few {
         };
 
         if (t0 < t1) {
-            pages.hold(a.c, it.seq, t0 >> shift, t1);
             load_k(t0);
             load_v(t0);
         }
@@ -211,15 +214,14 @@ template <typename T, bool FP8, int DP, int NQ> struct Few {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) kscale[j][r] = scale_of((uint32_t)__shfl((int)ks[j], g * 4 + r));
             }
-            if (more) {
-                if (((t + 2 * TOK - 1) >> shift) - pages.base >= 64) pages.hold(a.c, it.seq, (t + TOK) >> shift, t1);
-                load_k(t + TOK);
-            }
-
             bool gone = false;
 #pragma unroll
             for (int j = 0; j < NJ; ++j) gone |= vid[j] < 0;
             const bool masked = t + TOK > rg.full_hi || t + TOK > end || t < rg.full_lo || __any(gone);
+            if (more && ((t + 2 * TOK - 1) >> shift) - pages.base >= 64) pages.hold(a.c, it.seq, (t + TOK) >> shift, t1);
+            // (a masked step loads the next keys at its end: what it may have to do needs the registers)
+            if (more && !masked) load_k(t + TOK);
+
             float p[NQ][NJ][4];
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
@@ -270,7 +272,7 @@ template <typename T, bool FP8, int DP, int NQ> struct Few {
                             if (none) vs[j] = (vs[j] & ~(255u << (8 * r))) | (127u << (8 * r));
                         }
                     }
-                strange_values(t, see_lo, see_hi, vid, vr, vs, o);
+                clean_values(a, it, rg, t, see_lo, see_hi, vr, vs, o);
             }
             if constexpr (FP8) {        // a value's scale goes to its weight: exact, and one product instead of dim
 #pragma unroll
@@ -285,6 +287,7 @@ template <typename T, bool FP8, int DP, int NQ> struct Few {
             const Weights w = weights_of(p);
 #pragma unroll
             for (int x = 0; x < VDW; ++x) add_values(vr[x], w, o[x]);
+            if (more && masked) load_k(t + TOK);
             if (more) load_v(t + TOK);
         }
 
@@ -411,82 +414,78 @@ template <typename T, bool FP8, int DP, int NQ> struct Few {
     }
 
     // Values that are not finite, in a step whose tokens not every row sees: a weight of zero would not keep them out of the
-    // sums.  They are taken out of vr; rows that see one get it as the infinity or NaN that it is.
-    static __device__ __forceinline__ void strange_values(int t, const int (&see_lo)[NQ], const int (&see_hi)[NQ], const int (&vid)[NJ],
-                                                          uint32_t (&vr)[VDW][NJ * 4], uint32_t (&vs)[NJ], float4_t (&o)[VDW][NQ][PER])
+    // sums.  Rows that see one get it right away, as the infinity or NaN that it is; in vr they become zeros.
+    static __device__ __forceinline__ bool strange(uint32_t v)
     {
-        const int g = lane_id() >> 4;
-        // kind of value y of a dword of slot s: 0 finite, 1 inf, 2 -inf, 3 NaN
-        auto kind = [&](uint32_t dword, int s, int y) -> int {
-            if constexpr (FP8) {
-                const bool nan_scale = ((vs[s / 4] >> (8 * (s % 4))) & 255u) == 255u;
-                return nan_scale || ((dword >> (8 * y)) & 0x7fu) == 0x7fu ? 3 : 0;
-            } else if constexpr (F32) {
-                return (dword & 0x7f800000u) != 0x7f800000u ? 0 : (dword & 0x7fffffu) ? 3 : (dword >> 31) ? 2 : 1;
-            } else {
-                const uint32_t u = (dword >> (16 * y)) & 0xffffu;
-                return (u & 0x7f80u) != 0x7f80u ? 0 : (u & 0x7fu) ? 3 : (u >> 15) ? 2 : 1;
-            }
-        };
+        if constexpr (FP8) {        // a byte of 7f or ff: adding 1 to its low seven bits carries into the eighth
+            return (((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+        } else if constexpr (F32) {
+            return (v & 0x7f800000u) == 0x7f800000u;
+        } else {
+            return ((v & 0x7f80u) == 0x7f80u) | ((v & 0x7f800000u) == 0x7f800000u);
+        }
+    }
+    static __device__ __forceinline__ uint32_t finite_of(uint32_t v)
+    {
+        if constexpr (FP8) {
+            const uint32_t nan = ((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+            return v & ~(nan | (nan - (nan >> 7)));                      // (80 -> ff)
+        } else if constexpr (F32) {
+            return strange(v) ? 0u : v;
+        } else {
+            return ((v & 0x7f80u) == 0x7f80u ? 0u : v & 0xffffu) | ((v & 0x7f800000u) == 0x7f800000u ? 0u : v & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ void clean_values(const AttnArgs& a, const Item& it, const Range& rg, int t, const int (&see_lo)[NQ],
+                                                        const int (&see_hi)[NQ], uint32_t (&vr)[VDW][NJ * 4], uint32_t (&vs)[NJ],
+                                                        float4_t (&o)[VDW][NQ][PER])
+    {
         bool any = false;
 #pragma unroll
-        for (int x = 0; x < VDW; ++x)
+        for (int s = 0; s < NJ * 4; ++s) {
 #pragma unroll
-            for (int s = 0; s < NJ * 4; ++s)
-#pragma unroll
-                for (int y = 0; y < PER; ++y) any |= kind(vr[x][s], s, y) != 0;
-        if (!__any(any)) return;
-        // 1 where a row sees a token, as weights
-        float seen[NQ][NJ][4];
-#pragma unroll
-        for (int i = 0; i < NQ; ++i)
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int tok = t + j * 16 + g * 4 + r;
-                    seen[i][j][r] = vid[j] >= 0 && tok < see_hi[i] && tok >= see_lo[i] ? 1.0f : 0.0f;
-                }
-        const Weights w = weights_of(seen);
-#pragma unroll
-        for (int x = 0; x < VDW; ++x) {
-#pragma unroll 1
-            for (int what = 1; what <= 3; ++what) {
-                uint32_t mark[NJ * 4];
-#pragma unroll
-                for (int s = 0; s < NJ * 4; ++s) {
-                    mark[s] = 0;
-#pragma unroll
-                    for (int y = 0; y < PER; ++y)
-                        if (kind(vr[x][s], s, y) == what) mark[s] |= (FP8 ? 0x38u : F32 ? 0x3f800000u : 0x3f80u) << (y * (32 / PER));
-                }
-                float4_t hits[NQ][PER];
-#pragma unroll
-                for (int i = 0; i < NQ; ++i)
-#pragma unroll
-                    for (int y = 0; y < PER; ++y) hits[i][y] = float4_t{0, 0, 0, 0};
-                add_values(mark, w, hits);
-                const float worth = what == 1 ? __builtin_inff() : what == 2 ? -__builtin_inff() : __builtin_nanf("");
-#pragma unroll
-                for (int i = 0; i < NQ; ++i)
-#pragma unroll
-                    for (int y = 0; y < PER; ++y)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) o[x][i][y][r] += hits[i][y][r] > 0.5f ? worth : 0.0f;
-            }
-#pragma unroll
-            for (int s = 0; s < NJ * 4; ++s) {
-                uint32_t keep = 0;
-#pragma unroll
-                for (int y = 0; y < PER; ++y)
-                    if (kind(vr[x][s], s, y) == 0) keep |= (0xffffffffu >> (32 - 32 / PER)) << (y * (32 / PER));
-                vr[x][s] &= keep;
-            }
+            for (int x = 0; x < VDW; ++x) any |= strange(vr[x][s]);
+            if constexpr (FP8) any |= ((vs[s / 4] >> (8 * (s % 4))) & 255u) == 255u;
         }
-        if constexpr (FP8) {
+        if (!__any(any)) return;
 #pragma unroll
-            for (int s = 0; s < NJ * 4; ++s)
-                if (((vs[s / 4] >> (8 * (s % 4))) & 255u) == 255u) vs[s / 4] = (vs[s / 4] & ~(255u << (8 * (s % 4)))) | (127u << (8 * (s % 4)));
+        for (int s = 0; s < NJ * 4; ++s) {
+            bool drop = false;
+            if constexpr (FP8) {
+                drop = ((vs[s / 4] >> (8 * (s % 4))) & 255u) == 255u;
+                if (drop) vs[s / 4] = (vs[s / 4] & ~(255u << (8 * (s % 4)))) | (127u << (8 * (s % 4)));
+            }
+#pragma unroll
+            for (int x = 0; x < VDW; ++x) vr[x][s] = drop ? 0u : finite_of(vr[x][s]);
+        }
+        // (rare, so slow and small: the step's tokens one by one, read again, a lane the dimensions of its outputs)
+        const int g = lane_id() >> 4, D = EXACT ? DP : a.c.D;
+#pragma unroll 1
+        for (int tok = t; tok < t + TOK && tok < rg.hi; ++tok) {
+            const int p = tok >> a.c.page_shift;
+            const int id = p < a.c.max_pages ? a.c.table[(int64_t)it.seq * a.c.max_pages + p] : -1;
+            if (id < 0 || id >= a.c.n_pages) continue;
+            const int64_t row = page_row(id, a.c.Hk, it.head, a.c.page_shift, tok & ((1 << a.c.page_shift) - 1));
+            bool nan_row = false;
+            if constexpr (FP8) nan_row = a.c.vs[row] == 255;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = (g * 4 + r) * VW < D ? (g * 4 + r) * VW : 0;
+                uint32_t v[VDW];
+                load_dwords(a.c.v + (row * D + d) * ESZ, v);
+#pragma unroll
+                for (int x = 0; x < VDW; ++x)
+#pragma unroll
+                    for (int y = 0; y < PER; ++y) {
+                        float f;
+                        if constexpr (FP8) f = nan_row || ((v[x] >> (8 * y)) & 0x7fu) == 0x7fu ? __builtin_nanf("") : 0.0f;
+                        else f = __uint_as_float(F32 ? v[x] : y == 0 ? v[x] << 16 : v[x] & 0xffff0000u);
+                        const bool odd = (__float_as_uint(f) & 0x7f800000u) == 0x7f800000u;
+#pragma unroll
+                        for (int i = 0; i < NQ; ++i)
+                            if (odd && tok < see_hi[i] && tok >= see_lo[i]) o[x][i][y][r] += f;
+                    }
+            }
         }
     }
 };

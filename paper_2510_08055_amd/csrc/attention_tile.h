@@ -34,7 +34,7 @@ template <int N> __device__ __forceinline__ void load_lds_group(const uint32_t (
                      "v"(off[2]), "v"(off[3]), "s"(base), "s"(lds) : "memory");
 }
 
-template <bool FP8, int DP> struct Many {
+template <bool FP8, int DP, bool EXACT> struct Many {
     static constexpr int TOK = 64;
     static constexpr int ROWB = DP * 2;              // bytes of a token's row in LDS
     static constexpr int CH = DP / 8;                // its 16-byte chunks
@@ -93,7 +93,7 @@ template <bool FP8, int DP> struct Many {
         if (it.sub >= rg.pieces) return;
         const int lane = lane_id(), n = lane & 31, h = lane >> 5;
         const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-        const int D = a.c.D, shift = a.c.page_shift, Hk = a.c.Hk;
+        const int D = EXACT ? DP : a.c.D, shift = a.c.page_shift, Hk = a.c.Hk;
         const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_address(smem));
 
         const Row me = row_of(a, it, rg, rg.first + wave * 32 + n);
