@@ -410,10 +410,16 @@ class KVContext:
         except Exception:
             pass
 
-    def _stream(self):
+    def _call(self, name, *args):
+        """A call of the library on the context's GPU and that GPU's current stream."""
         if self.device.type != "cuda":
             raise ValueError(f"the kernels run on a GPU, not on {self.device}")
-        return _stream()
+        gpu = self.workspace.device.index
+        if torch._C._cuda_getDevice() != gpu:
+            with torch.cuda.device(gpu):
+                return self._call(name, *args)
+        # (the handle itself: torch.cuda.current_stream() takes 3 us to wrap it, as long as a launch)
+        _check(getattr(self.lib, name)(self._ctx, *args, torch._C._cuda_getCurrentRawStream(gpu)), name)
 
     def _dense(self, t, name, dtype, shape):
         if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != self.workspace.device:
@@ -461,7 +467,7 @@ class KVContext:
         T = k.shape[0]
         kp, ldk = self._rows(k, "k", T, self.kv_heads)
         vp, ldv = self._rows(v, "v", T, self.kv_heads)
-        _check(self.lib.moe_kv_append(self._ctx, kp, ldk, vp, ldv, T, pages, batch, self._stream()), "moe_kv_append")
+        self._call("moe_kv_append", kp, ldk, vp, ldv, T, pages, batch)
 
     def moe_kv_gather(self, pages, batch, T=None, k=None, v=None):
         """The rows' keys and values [T, kv_heads, dim]; T: the batch's rows, needed where no outputs are passed in."""
@@ -473,7 +479,7 @@ class KVContext:
         T = k.shape[0]
         kp, ldk = self._rows(k, "k", T, self.kv_heads)
         vp, ldv = self._rows(v, "v", T, self.kv_heads)
-        _check(self.lib.moe_kv_gather(self._ctx, pages, batch, T, kp, ldk, vp, ldv, self._stream()), "moe_kv_gather")
+        self._call("moe_kv_gather", pages, batch, T, kp, ldk, vp, ldv)
         return k, v
 
     def moe_paged_attention(self, q, pages, batch, causal=True, window=0, sinks=None, out=None, lse=None):
@@ -486,5 +492,5 @@ class KVContext:
         opt = CAttentionOptions(int(bool(causal)), int(window),
                                 self._dense(sinks, "sinks", torch.float32, (self.heads,)) if sinks is not None else None)
         lp = self._dense(lse, "lse", torch.float32, (T, self.heads)) if lse is not None else None
-        _check(self.lib.moe_paged_attention(self._ctx, qp, ldq, T, pages, batch, opt, op, ldo, lp, self._stream()), "moe_paged_attention")
+        self._call("moe_paged_attention", qp, ldq, T, pages, batch, opt, op, ldo, lp)
         return out

@@ -52,6 +52,7 @@ template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> hipError_t launc
     a.tile_rows = K::MANY ? kManyRows : a.few_rows;
     a.tile_tokens = a.tile_rows / a.G;
     a.g_magic = map_magic_of(a.G);
+    a.hk_magic = map_magic_of(a.c.Hk);
     // a block for every item there can be: a tile for a sequence and for tile_rows more packed rows; pieces are kFewItems and kTileItems
     // more at most (and a few for the rounding of their lengths), fewer where no history is long
     const int64_t tiles = (int64_t)(a.c.S < a.c.T ? a.c.S : a.c.T) + (int64_t)a.c.T * a.G / a.tile_rows;

@@ -144,7 +144,7 @@ template <typename T, bool FP8, int DP, int NQ, bool EXACT> struct Few {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     uint32_t raw[VDW];
-                    load_dwords(p + (int64_t)r * D * ESZ, raw);
+                    load_dwords<true>(p + (int64_t)r * D * ESZ, raw);
 #pragma unroll
                     for (int x = 0; x < VDW; ++x) vr[x][j * 4 + r] = raw[x];
                 }

@@ -59,23 +59,33 @@ __device__ __forceinline__ Seq shape_of(const AttnArgs& a, int lo, int hi, int k
 __device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
 __device__ __forceinline__ float last_lane(float v) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63)); }
 
+// v / d for d > 1, from magic = ceil(2^32 / d), which overshoots by one at most.
+__device__ __forceinline__ uint32_t divided(uint32_t v, uint32_t d, uint32_t magic)
+{
+    const uint32_t q = __umulhi(v, magic);
+    return q * d > v ? q - 1 : q;
+}
+
 struct PlanShared {
     float work[2][4];
     int sums[3][4], bad[4];
-    int found[10];
+    int found[9];
 };
 
 // The item of a block, the same in all of its threads.  A thread takes a sequence (256 at a time), so that the code is short: every
-// block of a launch runs it before it can load anything, and code that runs once costs its instruction misses.
+// block of a launch runs it before it can load anything, and code that runs once costs its instruction misses.  Up to 64 sequences
+// every wave does it for itself, and nothing goes through LDS.
 // Offsets that descend, or leave [0, T], would name rows twice or none: then there are no items at all.
 __device__ __forceinline__ Item find_item(const AttnArgs& a, int block, PlanShared& sh)
 {
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int S = a.c.S, Hk = a.c.Hk;
+    const bool alone = S <= 64;
+    const int me = alone ? lane : (int)threadIdx.x;
     Seq q;
     bool bad = false;
     auto load = [&](int b) {
-        const int s = b + (int)threadIdx.x;
+        const int s = b + me;
         const int lo = a.c.off[s < S ? s : S], hi = a.c.off[s < S ? s + 1 : S], kv = a.c.lens[s < S ? s : S - 1];
         bad |= (lo < 0) | (hi < lo) | (hi > a.c.T);
         q = shape_of(a, lo, bad ? lo : hi, kv);
@@ -89,18 +99,26 @@ __device__ __forceinline__ Item find_item(const AttnArgs& a, int block, PlanShar
     }
     few = wave_scan(few);
     many = wave_scan(many);
-    if (lane == 63) {
-        sh.work[0][wave] = few;
-        sh.work[1][wave] = many;
-    }
-    const bool any_bad = __any(bad);
-    if (lane == 0) sh.bad[wave] = any_bad;
-    __syncthreads();
+    bool any_bad = __any(bad);
     Item it;
     it.valid = false;
-    if (sh.bad[0] | sh.bad[1] | sh.bad[2] | sh.bad[3]) return it;
-    few = (sh.work[0][0] + sh.work[0][1] + sh.work[0][2] + sh.work[0][3]) * (float)Hk;
-    many = (sh.work[1][0] + sh.work[1][1] + sh.work[1][2] + sh.work[1][3]) * (float)Hk;
+    if (alone) {
+        few = last_lane(few);
+        many = last_lane(many);
+    } else {
+        if (lane == 63) {
+            sh.work[0][wave] = few;
+            sh.work[1][wave] = many;
+            sh.bad[wave] = any_bad;
+        }
+        __syncthreads();
+        any_bad = (sh.bad[0] | sh.bad[1] | sh.bad[2] | sh.bad[3]) != 0;
+        few = sh.work[0][0] + sh.work[0][1] + sh.work[0][2] + sh.work[0][3];
+        many = sh.work[1][0] + sh.work[1][1] + sh.work[1][2] + sh.work[1][3];
+    }
+    if (any_bad) return it;
+    few *= (float)Hk;
+    many *= (float)Hk;
     // A token costs an item of either kind about the same time (of a unit's share of the memory, or of its matrix cores).
     auto even = [](float work, int items, int least) {
         const float v = work * (1.0f / (float)items);
@@ -118,12 +136,17 @@ __device__ __forceinline__ Item find_item(const AttnArgs& a, int block, PlanShar
         count[1] = q.many ? 0 : n;
         need = pieces > 1 ? n * q.units : 0;
     };
-    int total[3] = {0, 0, 0}, incl[3], below[3];
-    // inclusive sums over the block's threads so far: incl (of the wave) + below (of the waves before)
+    int total[3] = {0, 0, 0}, incl[3], below[3] = {0, 0, 0};
+    // inclusive sums over the sequences so far: incl (of the wave) + below (of the waves before)
     auto scan = [&](int c0, int c1, int c2) {
         incl[0] = wave_scan(c0);
         incl[1] = wave_scan(c1);
         incl[2] = wave_scan(c2);
+        if (alone) {
+#pragma unroll
+            for (int k = 0; k < 3; ++k) total[k] = last_lane(incl[k]);
+            return;
+        }
         __syncthreads();
         if (lane == 63) {
 #pragma unroll
@@ -172,47 +195,61 @@ __device__ __forceinline__ Item find_item(const AttnArgs& a, int block, PlanShar
         block = (kind == 0 ? before : g - before) * 8 + block % 8;
     }
     if (block >= total[kind]) return it;
-    if (S > 256) total[0] = total[1] = total[2] = 0;
-    for (int b = 0; b < S; b += 256) {
-        int before = 0, slots = 0;
-        if (S > 256) {
-            before = total[kind];
-            slots = total[2];
-            load(b);
-            count_items();
-            scan(count[0], count[1], need);
+    int rem = 0, pc = 1;
+    auto found = [&](int b, int slots, auto put) {
+        const int n = count[kind], r = block - (below[kind] + incl[kind] - n);
+        const bool here = r >= 0 && r < n;
+        put(here, q.row0, q.n, q.kv, q.tiles, q.units, b + me, r, pieces, slots + below[2] + incl[2] - need);
+    };
+    if (alone) {
+        found(0, 0, [&](bool here, int row0, int n, int kv, int tiles, int units, int seq, int r, int p, int slot) {
+            const int src = __ffsll((long long)__ballot(here)) - 1;
+            auto get = [&](int v) { return __builtin_amdgcn_readlane(v, src); };
+            it.q.row0 = get(row0); it.q.n = get(n); it.q.kv = get(kv); it.q.tiles = get(tiles); it.q.units = get(units);
+            it.seq = get(seq); rem = get(r); pc = get(p); it.slot = get(slot);
+        });
+    } else {
+        if (S > 256) total[0] = total[1] = total[2] = 0;
+        for (int b = 0; b < S; b += 256) {
+            int slots = 0;
+            if (S > 256) {
+                const int before = total[kind];
+                slots = total[2];
+                load(b);
+                count_items();
+                scan(count[0], count[1], need);
+                below[kind] += before;
+            }
+            found(b, slots, [&](bool here, int row0, int n, int kv, int tiles, int units, int seq, int r, int p, int slot) {
+                if (here) {
+                    sh.found[0] = row0; sh.found[1] = n; sh.found[2] = kv; sh.found[3] = tiles; sh.found[4] = units;
+                    sh.found[5] = seq; sh.found[6] = r; sh.found[7] = p; sh.found[8] = slot;
+                }
+            });
+            if (S > 256 && block < total[kind]) break;
         }
-        const int n = count[kind], rem = block - (before + below[kind] + incl[kind] - n);
-        if (rem >= 0 && rem < n) {
-            sh.found[0] = q.row0; sh.found[1] = q.n; sh.found[2] = q.kv; sh.found[3] = q.tiles; sh.found[4] = q.units;
-            sh.found[5] = b + threadIdx.x; sh.found[6] = rem; sh.found[7] = pieces; sh.found[8] = slots + below[2] + incl[2] - need;
-        }
-        if (S > 256 && block < total[kind]) break;
+        __syncthreads();
+        auto get = [&](int i) { return __builtin_amdgcn_readfirstlane(sh.found[i]); };
+        it.q.row0 = get(0); it.q.n = get(1); it.q.kv = get(2); it.q.tiles = get(3); it.q.units = get(4);
+        it.seq = get(5); rem = get(6); pc = get(7); it.slot = get(8);
     }
-    __syncthreads();
-    auto get = [&](int i) { return __builtin_amdgcn_readfirstlane(sh.found[i]); };
-    it.q.row0 = get(0); it.q.n = get(1); it.q.kv = get(2); it.q.tiles = get(3); it.q.units = get(4);
     it.q.many = kind == 0;
-    it.seq = get(5);
-    int rem = get(6);
-    const int pc = get(7);
     // heads side by side (they go to different XCDs, and the tiles of a head to the same ones), long tiles first
-    it.head = rem % Hk;
-    rem /= Hk;
-    it.sub = rem % pc;
-    it.tile = it.q.tiles - 1 - rem / pc;
+    const int across = Hk == 1 ? rem : (int)divided((uint32_t)rem, (uint32_t)Hk, a.hk_magic);
+    it.head = rem - across * Hk;
+    const int down = pc == 1 ? across : across / pc;
+    it.sub = across - down * pc;
+    it.tile = it.q.tiles - 1 - down;
     it.piece = pc == 1 ? 0 : it.q.many ? many_piece : few_piece;
-    it.slot = get(8) + (it.tile * Hk + it.head) * pc * it.q.units;
+    it.slot += (it.tile * Hk + it.head) * pc * it.q.units;
     it.valid = true;
     return it;
 }
 
-// The new token of packed row r: r / G, from ceil(2^32 / G) (one too high at most).
+// The new token of packed row r: r / G.
 __device__ __forceinline__ int token_of(const AttnArgs& a, int r)
 {
-    if (a.G == 1) return r;
-    const uint32_t q = __umulhi((uint32_t)r, a.g_magic);
-    return (int)(q * (uint32_t)a.G > (uint32_t)r ? q - 1 : q);
+    return a.G == 1 ? r : (int)divided((uint32_t)r, (uint32_t)a.G, a.g_magic);
 }
 
 // The tokens that a tile's rows see: all rows those of [full_lo, full_hi), some row those of [lo, hi); lo is a multiple of 32.
@@ -284,19 +321,26 @@ struct Entries {
     }
 };
 
-// N consecutive dwords, as wide as they can be loaded.
-template <int N> __device__ __forceinline__ void load_dwords(const char* p, uint32_t (&x)[N])
+// N consecutive dwords, as wide as they can be loaded.  STREAM: bytes that nobody asks for again.
+typedef uint32_t uint32x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t uint32x4_t __attribute__((ext_vector_type(4)));
+template <bool STREAM, typename V> __device__ __forceinline__ V load_as(const char* p)
+{
+    if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+    else return *reinterpret_cast<const V*>(p);
+}
+template <bool STREAM = false, int N> __device__ __forceinline__ void load_dwords(const char* p, uint32_t (&x)[N])
 {
     if constexpr (N == 1) {
-        x[0] = *reinterpret_cast<const uint32_t*>(p);
+        x[0] = load_as<STREAM, uint32_t>(p);
     } else if constexpr (N == 2) {
-        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        const uint32x2_t v = load_as<STREAM, uint32x2_t>(p);
         x[0] = v.x; x[1] = v.y;
     } else {
         static_assert(N % 4 == 0, "whole 16-byte pieces");
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) {
-            const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+            const uint32x4_t v = load_as<STREAM, uint32x4_t>(p + 16 * i);
             x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
         }
     }

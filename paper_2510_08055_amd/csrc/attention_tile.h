@@ -80,7 +80,6 @@ template <bool FP8, int DP, bool EXACT> struct Many {
         const uint2 lo = read_transposed(v_at[0][x] + k * 16 * ROWB), hi = read_transposed(v_at[1][x] + k * 16 * ROWB);
         return __builtin_bit_cast(bf16x8_t, make_uint4(lo.x, lo.y, hi.x, hi.y));
     }
-    typedef uint32_t uint32x4_t __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) uint32x4_t lds_chunk_t;
     static __device__ __forceinline__ bf16x8_t read_keys(uint32_t lds)
     {
