@@ -292,6 +292,7 @@ template <typename T, bool FP8, int DP, int NQ, bool EXACT> struct Few {
         }
 
         // a wave's sums, then the block's
+        const Parts parts = parts_of(a, D);
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
             l[i] = sum_over_tokens(l[i]);
@@ -325,7 +326,7 @@ template <typename T, bool FP8, int DP, int NQ, bool EXACT> struct Few {
                 for (int w = 0; w < 4; ++w) M = fmaxf(M, sh.stats[0][w][i * 16 + q]);
 #pragma unroll
                 for (int w = 0; w < 4; ++w) L += sh.stats[1][w][i * 16 + q] * __builtin_amdgcn_exp2f(sh.stats[0][w][i * 16 + q] - M);
-                const int64_t part = (int64_t)(it.slot + it.sub * it.q.units + i) * 16 + q;
+                const int part = (it.slot + it.sub * it.q.units + i) * 16 + q;
                 const Finish fin = finish_row(a, r.head, M, L);
                 const float to = rg.pieces > 1 ? 1.0f : fin.factor;
                 for (int d = (threadIdx.x & 15) * 4; d < D; d += 64) {
@@ -336,8 +337,8 @@ template <typename T, bool FP8, int DP, int NQ, bool EXACT> struct Few {
                         v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
                     }
                     const float4 res = make_float4(v[0] * to, v[1] * to, v[2] * to, v[3] * to);
-                    if (rg.pieces > 1) store_part(a, part, d, res);
-                    else store_out<T>(a, r.row, r.head, d, res);
+                    if (rg.pieces > 1) store_part(parts, part, d, res);
+                    else store_out<T>(a, r.row, r.head, D, d, res);
                 }
                 if ((threadIdx.x & 15) == 0) {
                     if (rg.pieces > 1) store_part_stats(a, part, M, L);
@@ -345,7 +346,7 @@ template <typename T, bool FP8, int DP, int NQ, bool EXACT> struct Few {
                 }
             }
         }
-        if (rg.pieces > 1) join_pieces<T, DP>(a, it, rg, &sh.flag);
+        if (rg.pieces > 1) join_pieces<T, DP, NQ>(a, it, rg, D, &sh.flag);
     }
 
     // The weights as the second product's operand.

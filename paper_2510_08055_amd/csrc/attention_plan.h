@@ -366,84 +366,111 @@ __device__ __forceinline__ Finish finish_row(const AttnArgs& a, int head, float 
     return f;
 }
 // Four dimensions from d on of a finished row.
-template <typename T> __device__ __forceinline__ void store_out(const AttnArgs& a, int row, int head, int d, float4 o)
+template <typename T> __device__ __forceinline__ void store_out(const AttnArgs& a, int row, int head, int D, int d, float4 o)
 {
-    T* dst = static_cast<T*>(a.out) + (int64_t)row * a.ldo + head * a.c.D + d;
+    T* dst = static_cast<T*>(a.out) + (int64_t)row * a.ldo + head * D + d;
     if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
     else *reinterpret_cast<float4*>(dst) = o;
 }
 
 // ---- partial results of a piece: per row its output sums, maximum and sum, to be read by the block that ends the tile ----
-__device__ __forceinline__ uint64_t two(float x, float y) { return (uint64_t)__float_as_uint(x) | (uint64_t)__float_as_uint(y) << 32; }
-__device__ __forceinline__ float2 two_of(uint64_t v) { return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))); }
-__device__ __forceinline__ void store_part(const AttnArgs& a, int64_t row, int d, float4 o)
+// Like store_shared and load_shared, 16 bytes at a time: past the caches of one XCD (the buffer instructions take that as a constant,
+// and keep to the workspace by themselves).
+constexpr int kShared = 1 << 4;      // sc1
+struct Parts {
+    __amdgpu_buffer_rsrc_t sums;
+    int D;
+};
+__device__ __forceinline__ Parts parts_of(const AttnArgs& a, int D)
 {
-    uint64_t* dst = reinterpret_cast<uint64_t*>(a.part + row * a.c.D + d);
-    store_shared(dst, two(o.x, o.y));
-    store_shared(dst + 1, two(o.z, o.w));
+    return Parts{__builtin_amdgcn_make_buffer_rsrc(a.part, 0, kPartUnits * 16 * D * (int)sizeof(float), 0x00020000), D};
 }
-__device__ __forceinline__ void store_part_stats(const AttnArgs& a, int64_t row, float m, float l)
+__device__ __forceinline__ void store_part(const Parts& p, int row, int d, float4 o)
 {
-    store_shared(reinterpret_cast<uint64_t*>(a.part_stats + row), two(m, l));
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint32x4_t, o), p.sums, (row * p.D + d) * (int)sizeof(float), 0, kShared);
+}
+__device__ __forceinline__ float4 load_part(const Parts& p, int row, int d)
+{
+    return __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(p.sums, (row * p.D + d) * (int)sizeof(float), 0, kShared));
+}
+__device__ __forceinline__ void store_part_stats(const AttnArgs& a, int row, float m, float l)
+{
+    store_shared(reinterpret_cast<uint64_t*>(a.part_stats + row), (uint64_t)__float_as_uint(m) | (uint64_t)__float_as_uint(l) << 32);
+}
+__device__ __forceinline__ float2 load_part_stats(const AttnArgs& a, int row)
+{
+    const uint64_t v = load_shared(reinterpret_cast<const uint64_t*>(a.part_stats + row));
+    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 
 // Every thread of a block that has stored its piece of a tile calls it; the block that ends the tile joins its pieces, in their order (so
 // the result does not depend on who came last).  Sixteen lanes to a row, four pieces in flight.
-template <typename T, int DP> __device__ __forceinline__ void join_pieces(const AttnArgs& a, const Item& it, const Range& rg, int32_t* flag)
+template <typename T, int DP, int UNITS>
+__device__ __forceinline__ void join_pieces(const AttnArgs& a, const Item& it, const Range& rg, int D, int32_t* flag)
 {
     if (!last_to_arrive(a.tickets + it.slot, (uint32_t)rg.pieces, flag)) return;
-    constexpr int ND = (DP + 63) / 64;
-    const int units = it.q.units, D = a.c.D, d0 = (threadIdx.x & 15) * 4;
-    for (int u = 0; u < units; ++u) {
-        const int q = threadIdx.x >> 4, r = rg.first + u * 16 + q;
-        if (r >= rg.rows) return;
-        float M = kLowest, L = 0;
-        float4 o[ND];
+    constexpr int ND = (DP + 63) / 64, AT_ONCE = UNITS > 1 && ND <= 2 ? 2 : 1;      // units
+    const int units = it.q.units, d0 = (threadIdx.x & 15) * 4, q = threadIdx.x >> 4;
+    const Parts parts = parts_of(a, D);
+    for (int u0 = 0; u0 < units; u0 += AT_ONCE) {
+        if (rg.first + u0 * 16 >= rg.rows) return;
+        float M[AT_ONCE], L[AT_ONCE];
+        float4 o[AT_ONCE][ND];
 #pragma unroll
-        for (int k = 0; k < ND; ++k) o[k] = make_float4(0, 0, 0, 0);
+        for (int u = 0; u < AT_ONCE; ++u) {
+            M[u] = kLowest;
+            L[u] = 0;
+#pragma unroll
+            for (int k = 0; k < ND; ++k) o[u][k] = make_float4(0, 0, 0, 0);
+        }
         for (int c0 = 0; c0 < rg.pieces; c0 += 4) {
-            float2 st[4];
-            uint64_t x[4][ND][2];
+            float2 st[4][AT_ONCE];
+            float4 x[4][AT_ONCE][ND];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int at = c0 + c < rg.pieces ? c0 + c : rg.pieces - 1;
-                const int64_t row = (int64_t)(it.slot + at * units + u) * 16 + q;
-                st[c] = two_of(load_shared(reinterpret_cast<const uint64_t*>(a.part_stats + row)));
+            for (int c = 0; c < 4; ++c)
 #pragma unroll
-                for (int k = 0; k < ND; ++k) {
-                    const uint64_t* src = reinterpret_cast<const uint64_t*>(a.part + row * D + (d0 + k * 64 < D ? d0 + k * 64 : 0));
-                    x[c][k][0] = load_shared(src);
-                    x[c][k][1] = load_shared(src + 1);
+                for (int u = 0; u < AT_ONCE; ++u) {
+                    const int at = c0 + c < rg.pieces ? c0 + c : rg.pieces - 1;
+                    const int row = (it.slot + at * units + u0 + u) * 16 + q;
+                    st[c][u] = load_part_stats(a, row);
+#pragma unroll
+                    for (int k = 0; k < ND; ++k) x[c][u][k] = load_part(parts, row, d0 + k * 64 < D ? d0 + k * 64 : 0);
                 }
-            }
-            float top = M;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) top = fmaxf(top, st[c].x);
-            const float back = __builtin_amdgcn_exp2f(M - top);
-            M = top;
-            L *= back;
+            for (int u = 0; u < AT_ONCE; ++u) {
+                float top = M[u];
 #pragma unroll
-            for (int k = 0; k < ND; ++k) { o[k].x *= back; o[k].y *= back; o[k].z *= back; o[k].w *= back; }
+                for (int c = 0; c < 4; ++c) top = fmaxf(top, st[c][u].x);
+                const float back = __builtin_amdgcn_exp2f(M[u] - top);
+                M[u] = top;
+                L[u] *= back;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                if (c0 + c < rg.pieces) {
-                    const float f = __builtin_amdgcn_exp2f(st[c].x - top);
-                    L += st[c].y * f;
+                for (int k = 0; k < ND; ++k) { o[u][k].x *= back; o[u][k].y *= back; o[u][k].z *= back; o[u][k].w *= back; }
 #pragma unroll
-                    for (int k = 0; k < ND; ++k) {
-                        const float2 lo = two_of(x[c][k][0]), hi = two_of(x[c][k][1]);
-                        o[k].x += lo.x * f; o[k].y += lo.y * f; o[k].z += hi.x * f; o[k].w += hi.y * f;
+                for (int c = 0; c < 4; ++c) {
+                    if (c0 + c < rg.pieces) {
+                        const float f = __builtin_amdgcn_exp2f(st[c][u].x - top);
+                        L[u] += st[c][u].y * f;
+#pragma unroll
+                        for (int k = 0; k < ND; ++k) {
+                            const float4 v = x[c][u][k];
+                            o[u][k].x += v.x * f; o[u][k].y += v.y * f; o[u][k].z += v.z * f; o[u][k].w += v.w * f;
+                        }
                     }
                 }
             }
         }
-        const Row row = row_of(a, it, rg, r);
-        const Finish f = finish_row(a, row.head, M, L);
 #pragma unroll
-        for (int k = 0; k < ND; ++k)
-            if (d0 + k * 64 < D)
-                store_out<T>(a, row.row, row.head, d0 + k * 64, make_float4(o[k].x * f.factor, o[k].y * f.factor, o[k].z * f.factor, o[k].w * f.factor));
-        if (a.lse && d0 == 0) a.lse[(int64_t)row.row * a.Hq + row.head] = f.lse;
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const Row row = row_of(a, it, rg, rg.first + (u0 + u) * 16 + q);
+            if (!row.there || u0 + u >= units) continue;
+            const Finish f = finish_row(a, row.head, M[u], L[u]);
+#pragma unroll
+            for (int k = 0; k < ND; ++k)
+                if (d0 + k * 64 < D)
+                    store_out<T>(a, row.row, row.head, D, d0 + k * 64, make_float4(o[u][k].x * f.factor, o[u][k].y * f.factor, o[u][k].z * f.factor, o[u][k].w * f.factor));
+            if (a.lse && d0 == 0) a.lse[(int64_t)row.row * a.Hq + row.head] = f.lse;
+        }
     }
 }
 

@@ -330,31 +330,41 @@ template <bool FP8, int DP, bool EXACT> struct Many {
             cur = next;
         }
 
-        // results
+        // Results: a wave turns its 32 rows by way of LDS, so that they leave in whole rows.  Chunk c (four dimensions) of row q
+        // sits in place c ^ (q % chunks).
         l = swap_sum(l);
         const Finish fin = finish_row(a, me.head, m, l);
         const float f = rg.pieces > 1 ? 1.0f : fin.factor;
-        const int64_t part = (int64_t)(it.slot + it.sub * it.q.units) * 16 + wave * 32 + n;
-        if (me.there) {
+        const int part = (it.slot + it.sub * it.q.units) * 16 + wave * 32;
+        if (me.there && h == 0) {
+            if (rg.pieces > 1) store_part_stats(a, part + n, m, l);
+            else if (a.lse) a.lse[(int64_t)me.row * a.Hq + me.head] = fin.lse;
+        }
+        constexpr int OC = DP / 4, RPI = 64 / (OC < 64 ? OC : 64);     // chunks of a row, rows to 64 lanes
+        __syncthreads();                                             // (the stages are no longer read)
+        char* mine = smem + wave * 32 * DP * 4;
 #pragma unroll
-            for (int x = 0; x < NB; ++x)
+        for (int x = 0; x < NB; ++x)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int d = x * 32 + r * 8 + h * 4;
-                    const float4 v = make_float4(o[x][4 * r] * f, o[x][4 * r + 1] * f, o[x][4 * r + 2] * f, o[x][4 * r + 3] * f);
-                    if (d < D) {
-                        if (rg.pieces > 1) store_part(a, part, d, v);
-                        else store_out<bf16_t>(a, me.row, me.head, d, v);
-                    }
-                }
-            if (h == 0) {
-                if (rg.pieces > 1) store_part_stats(a, part, m, l);
-                else if (a.lse) a.lse[(int64_t)me.row * a.Hq + me.head] = fin.lse;
+            for (int r = 0; r < 4; ++r)
+                *reinterpret_cast<float4*>(mine + n * DP * 4 + (((x * 8 + r * 2 + h) ^ (n & (OC - 1))) * 16)) =
+                    make_float4(o[x][4 * r] * f, o[x][4 * r + 1] * f, o[x][4 * r + 2] * f, o[x][4 * r + 3] * f);
+        __builtin_amdgcn_wave_barrier();                             // (a wave's LDS operations keep their order)
+        const Parts parts = parts_of(a, D);
+        const int c = lane % OC;
+#pragma unroll
+        for (int i = 0; i < 32 / RPI; ++i) {
+            const int q = i * RPI + lane / OC;
+            const float4 v = *reinterpret_cast<const float4*>(mine + q * DP * 4 + ((c ^ (q & (OC - 1))) * 16));
+            const Row row = row_of(a, it, rg, rg.first + wave * 32 + q);
+            if (row.there && c * 4 < D) {
+                if (rg.pieces > 1) store_part(parts, part + q, c * 4, v);
+                else store_out<bf16_t>(a, row.row, row.head, D, c * 4, v);
             }
         }
         if (rg.pieces > 1) {
             __syncthreads();                                         // the flag shares the stages' memory
-            join_pieces<bf16_t, DP>(a, it, rg, reinterpret_cast<int32_t*>(smem));
+            join_pieces<bf16_t, DP, 8>(a, it, rg, D, reinterpret_cast<int32_t*>(smem));
         }
     }
 
