@@ -26,46 +26,48 @@ __device__ __forceinline__ int find_sequence(const int32_t* __restrict__ off, in
     return lo + __popcll(__ballot(below));
 }
 
-// Where the row of lane's vector lies: its row index among the pages' rows, or -1 where the token is not there.
-// first: the wave's first row; rows of a wave differ by little, so a lane steps on from that row's sequence.
-__device__ __forceinline__ int64_t find_slot(const KVView& c, int first, int row, int h)
+// A wave's share of a batch: 64 / LPR consecutive rows, LPR lanes to each, and R of a row's 2 Hk vectors (keys of all heads, then
+// values).  Consecutive tokens of a head lie side by side in a page, so a wave reads (or writes) whole stretches of it and whole
+// vectors of the rows, and a row's place is looked up once for its R vectors, all of which are in flight together.
+constexpr int R = 4;
+struct Share {
+    int row, first;      // this lane's row, the wave's first
+    int piece;           // the lane's place among its vector's lanes
+    int r0;              // the first vector
+    bool valid;
+};
+template <int LPR> __device__ __forceinline__ Share my_share(const KVView& c)
 {
-    int s = find_sequence(c.off, c.S, first);
-    while (s < c.S && c.off[s + 1] <= row) ++s;
+    const int parts = (2 * c.Hk + R - 1) / R;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+    const int group = wave / parts;
+    Share s;
+    s.first = group * (64 / LPR);
+    s.row = s.first + lane_id() / LPR;
+    s.piece = lane_id() % LPR;
+    s.r0 = (wave - group * parts) * R;
+    s.valid = s.row < c.T;
+    return s;
+}
+
+// Where the row's token lies: the index of its row for head 0 among the pages' rows, or -1 where it is not there.
+__device__ __forceinline__ int64_t find_slot(const KVView& c, const Share& t)
+{
+    int s = find_sequence(c.off, c.S, t.first);
+    while (s < c.S && c.off[s + 1] <= t.row) ++s;      // (rows of a wave differ by little)
     if (s >= c.S) return -1;
     const int len = c.lens[s];
-    const int pos = (len > 0 ? len : 0) - (c.off[s + 1] - row);
+    const int pos = (len > 0 ? len : 0) - (c.off[s + 1] - t.row);
     const int p = pos >> c.page_shift;
     if (pos < 0 || p >= c.max_pages) return -1;
     const int id = c.table[(int64_t)s * c.max_pages + p];
     if (id < 0 || id >= c.n_pages) return -1;
-    return page_row(id, c.Hk, h, c.page_shift, pos & ((1 << c.page_shift) - 1));
+    return page_row(id, c.Hk, 0, c.page_shift, pos & ((1 << c.page_shift) - 1));
 }
 
-struct Vec {
-    int row, h;      // row of the batch, key/value head
-    bool value;      // a row of v
-    int first;       // row of the wave's first vector
-    int piece;       // the lane's place among the vector's lanes
-    bool valid;
-};
-// The vectors (row, k or v, head) of a batch in that order, LPR lanes to each.
-template <int LPR> __device__ __forceinline__ Vec my_vector(const KVView& c)
-{
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t vec = at / LPR;
-    const int64_t vec0 = (at - lane_id()) / LPR;
-    const int per_row = 2 * c.Hk;
-    Vec v;
-    v.piece = (int)(at % LPR);
-    v.row = (int)(vec / per_row);
-    const int r = (int)(vec - (int64_t)v.row * per_row);
-    v.value = r >= c.Hk;
-    v.h = v.value ? r - c.Hk : r;
-    v.first = __builtin_amdgcn_readfirstlane((int)(vec0 / per_row));
-    v.valid = v.row < c.T;
-    return v;
-}
+// Vector r of a row: of the values?, and its head.
+__device__ __forceinline__ bool is_value(const KVView& c, int r) { return r >= c.Hk; }
+__device__ __forceinline__ int head_of(const KVView& c, int r) { return r >= c.Hk ? r - c.Hk : r; }
 
 template <typename T> __device__ __forceinline__ void load8(const T* p, float (&x)[8])
 {
@@ -88,96 +90,144 @@ template <typename T> __device__ __forceinline__ void load8(const T* p, float (&
 template <int LPR> __global__ __launch_bounds__(256) void append_kernel(KVView c, const char* __restrict__ k, int64_t ldk,
                                                                         const char* __restrict__ v, int64_t ldv, int esz)
 {
-    const Vec t = my_vector<LPR>(c);
+    const Share t = my_share<LPR>(c);
     const int bytes = c.D * esz;
     const bool mine = t.valid && t.piece * 16 < bytes;
-    uint4 x = {};
-    if (mine) {
-        const char* src = t.value ? v + (int64_t)t.row * ldv * esz : k + (int64_t)t.row * ldk * esz;
-        x = *reinterpret_cast<const uint4*>(src + (int64_t)t.h * bytes + t.piece * 16);
+    uint4 x[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int r = t.r0 + i;
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (mine && r < 2 * c.Hk) {
+            const char* src = is_value(c, r) ? v + (int64_t)t.row * ldv * esz : k + (int64_t)t.row * ldk * esz;
+            x[i] = *reinterpret_cast<const uint4*>(src + (int64_t)head_of(c, r) * bytes + t.piece * 16);
+        }
     }
-    const int64_t at = find_slot(c, t.first, t.row, t.h);
-    if (mine && at >= 0) *reinterpret_cast<uint4*>((t.value ? c.v : c.k) + at * bytes + t.piece * 16) = x;
+    const int64_t at = find_slot(c, t);
+    if (!mine || at < 0) return;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int r = t.r0 + i;
+        if (r < 2 * c.Hk)
+            *reinterpret_cast<uint4*>((is_value(c, r) ? c.v : c.k) + (at + ((int64_t)head_of(c, r) << c.page_shift)) * bytes + t.piece * 16) = x[i];
+    }
 }
 
 // As FP8 codes: 8 elements to a lane.
 template <typename T, int LPR> __global__ __launch_bounds__(256) void append_fp8_kernel(KVView c, const T* __restrict__ k, int64_t ldk,
                                                                                         const T* __restrict__ v, int64_t ldv)
 {
-    const Vec t = my_vector<LPR>(c);
+    const Share t = my_share<LPR>(c);
     const bool mine = t.valid && t.piece * 8 < c.D;
-    float x[8] = {};
-    if (mine) load8((t.value ? v + (int64_t)t.row * ldv : k + (int64_t)t.row * ldk) + t.h * c.D + t.piece * 8, x);
-    const int64_t at = find_slot(c, t.first, t.row, t.h);
-    // |x| as integers: they order like the values, and everything that is not finite comes last
-    uint32_t top = 0;
+    float x[R][8] = {};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t a = __float_as_uint(x[i]) & 0x7fffffffu;
-        top = a > top ? a : top;
+    for (int i = 0; i < R; ++i) {
+        const int r = t.r0 + i;
+        if (mine && r < 2 * c.Hk)
+            load8((is_value(c, r) ? v + (int64_t)t.row * ldv : k + (int64_t)t.row * ldk) + head_of(c, r) * c.D + t.piece * 8, x[i]);
     }
+    const int64_t at = find_slot(c, t);
 #pragma unroll
-    for (int d = 1; d < LPR; d *= 2) {
-        const uint32_t o = (uint32_t)__shfl_xor((int)top, d);
-        top = o > top ? o : top;
-    }
-    // amax = m 2^(E - 126) with m in [1/2, 1): e = E - 126 - 9 if m <= 448 / 512, one more otherwise
-    const bool bad = top >= 0x7f800000u;
-    int e = (int)(top >> 23) - 135 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
-    e = e < -100 ? -100 : e;
-    if (top == 0) e = -9;
-    if (!mine || at < 0) return;
-    uint32_t lo = 0, hi = 0;
-    if (bad) {
-        lo = hi = 0x7f7f7f7fu;
-    } else {
-        // (a power of two is exact, except where it takes a value below the smallest normal one, far below the smallest code)
+    for (int i = 0; i < R; ++i) {
+        const int r = t.r0 + i;
+        // |x| as integers: they order like the values, and everything that is not finite comes last
+        uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_ldexpf(x[i], -e);
-        lo = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
-        lo = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], (int)lo, true);
-        hi = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[4], x[5], 0, false);
-        hi = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[6], x[7], (int)hi, true);
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t a = __float_as_uint(x[i][e]) & 0x7fffffffu;
+            top = a > top ? a : top;
+        }
+#pragma unroll
+        for (int d = 1; d < LPR; d *= 2) {
+            const uint32_t o = (uint32_t)__shfl_xor((int)top, d);
+            top = o > top ? o : top;
+        }
+        if (!mine || at < 0 || r >= 2 * c.Hk) continue;
+        // amax = m 2^(E - 126) with m in [1/2, 1): e = E - 126 - 9 if m <= 448 / 512, one more otherwise
+        const bool bad = top >= 0x7f800000u;
+        int e = (int)(top >> 23) - 135 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+        e = e < -100 ? -100 : e;
+        if (top == 0) e = -9;
+        uint32_t lo = 0x7f7f7f7fu, hi = 0x7f7f7f7fu;
+        if (!bad) {
+            // (a power of two is exact, except where it takes a value below the smallest normal one, far below the smallest code)
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_ldexpf(x[i][j], -e);
+            lo = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+            lo = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], (int)lo, true);
+            hi = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false);
+            hi = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], (int)hi, true);
+        }
+        const int64_t to = at + ((int64_t)head_of(c, r) << c.page_shift);
+        *reinterpret_cast<uint2*>((is_value(c, r) ? c.v : c.k) + to * c.D + t.piece * 8) = make_uint2(lo, hi);
+        if (t.piece == 0) (is_value(c, r) ? c.vs : c.ks)[to] = (uint8_t)(bad ? 255 : e + 127);
     }
-    *reinterpret_cast<uint2*>((t.value ? c.v : c.k) + at * c.D + t.piece * 8) = make_uint2(lo, hi);
-    if (t.piece == 0) (t.value ? c.vs : c.ks)[at] = (uint8_t)(bad ? 255 : e + 127);
 }
 
 template <int LPR> __global__ __launch_bounds__(256) void gather_kernel(KVView c, char* __restrict__ k, int64_t ldk, char* __restrict__ v,
                                                                         int64_t ldv, int esz)
 {
-    const Vec t = my_vector<LPR>(c);
+    const Share t = my_share<LPR>(c);
     const int bytes = c.D * esz;
-    const int64_t at = find_slot(c, t.first, t.row, t.h);
+    const int64_t at = find_slot(c, t);
     if (!t.valid || t.piece * 16 >= bytes) return;
-    uint4 x = {};
-    if (at >= 0) x = *reinterpret_cast<const uint4*>((t.value ? c.v : c.k) + at * bytes + t.piece * 16);
-    char* dst = t.value ? v + (int64_t)t.row * ldv * esz : k + (int64_t)t.row * ldk * esz;
-    *reinterpret_cast<uint4*>(dst + (int64_t)t.h * bytes + t.piece * 16) = x;
+    uint4 x[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int r = t.r0 + i;
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (at >= 0 && r < 2 * c.Hk)
+            x[i] = *reinterpret_cast<const uint4*>((is_value(c, r) ? c.v : c.k) + (at + ((int64_t)head_of(c, r) << c.page_shift)) * bytes + t.piece * 16);
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int r = t.r0 + i;
+        if (r >= 2 * c.Hk) break;
+        char* dst = is_value(c, r) ? v + (int64_t)t.row * ldv * esz : k + (int64_t)t.row * ldk * esz;
+        *reinterpret_cast<uint4*>(dst + (int64_t)head_of(c, r) * bytes + t.piece * 16) = x[i];
+    }
 }
 
 template <typename T, int LPR> __global__ __launch_bounds__(256) void gather_fp8_kernel(KVView c, T* __restrict__ k, int64_t ldk,
                                                                                         T* __restrict__ v, int64_t ldv)
 {
-    const Vec t = my_vector<LPR>(c);
-    const int64_t at = find_slot(c, t.first, t.row, t.h);
+    const Share t = my_share<LPR>(c);
+    const int64_t at = find_slot(c, t);
     if (!t.valid || t.piece * 8 >= c.D) return;
-    float x[8] = {};
-    if (at >= 0) {
-        const uint2 w = *reinterpret_cast<const uint2*>((t.value ? c.v : c.k) + at * c.D + t.piece * 8);
-        const float s = scale_of((t.value ? c.vs : c.ks)[at]);
-        const hw_float2_t a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.x, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.x, true);
-        const hw_float2_t d = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.y, false), e = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.y, true);
-        x[0] = a[0] * s; x[1] = a[1] * s; x[2] = b[0] * s; x[3] = b[1] * s;
-        x[4] = d[0] * s; x[5] = d[1] * s; x[6] = e[0] * s; x[7] = e[1] * s;
+    uint2 w[R];
+    uint32_t sb[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int r = t.r0 + i;
+        w[i] = make_uint2(0, 0);
+        sb[i] = 127;
+        if (at >= 0 && r < 2 * c.Hk) {
+            const int64_t from = at + ((int64_t)head_of(c, r) << c.page_shift);
+            w[i] = *reinterpret_cast<const uint2*>((is_value(c, r) ? c.v : c.k) + from * c.D + t.piece * 8);
+            sb[i] = (is_value(c, r) ? c.vs : c.ks)[from];
+        }
     }
-    T* dst = (t.value ? v + (int64_t)t.row * ldv : k + (int64_t)t.row * ldk) + t.h * c.D + t.piece * 8;
-    if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                                                    pack_bf16x2(x[6], x[7]));
-    } else {
-        reinterpret_cast<float4*>(dst)[0] = make_float4(x[0], x[1], x[2], x[3]);
-        reinterpret_cast<float4*>(dst)[1] = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int r = t.r0 + i;
+        if (r >= 2 * c.Hk) break;
+        const float s = scale_of(sb[i]);
+        float x[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int u = (int)(h == 0 ? w[i].x : w[i].y);
+            const hw_float2_t a = __builtin_amdgcn_cvt_pk_f32_fp8(u, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(u, true);
+            x[4 * h] = a[0] * s; x[4 * h + 1] = a[1] * s; x[4 * h + 2] = b[0] * s; x[4 * h + 3] = b[1] * s;
+        }
+        T* dst = (is_value(c, r) ? v + (int64_t)t.row * ldv : k + (int64_t)t.row * ldk) + head_of(c, r) * c.D + t.piece * 8;
+        if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                                                        pack_bf16x2(x[6], x[7]));
+        } else {
+            reinterpret_cast<float4*>(dst)[0] = make_float4(x[0], x[1], x[2], x[3]);
+            reinterpret_cast<float4*>(dst)[1] = make_float4(x[4], x[5], x[6], x[7]);
+        }
     }
 }
 
@@ -191,7 +241,8 @@ template <typename F> hipError_t by_lanes(int n, F f)
 }
 inline unsigned blocks_for(const KVView& c, int lanes)
 {
-    return (unsigned)(((int64_t)c.T * 2 * c.Hk * lanes + 255) / 256);
+    const int64_t groups = ((int64_t)c.T * lanes + 63) / 64, parts = (2 * c.Hk + R - 1) / R;
+    return (unsigned)((groups * parts + 3) / 4);
 }
 
 }  // namespace
