@@ -51,20 +51,24 @@ template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> hipError_t launc
     a.few_rows = K::NQ * 16;
     a.tile_rows = K::MANY ? kManyRows : a.few_rows;
     a.tile_tokens = a.tile_rows / a.G;
+    int units = 0;
+    hipError_t e = compute_units(&units);
+    if (e != hipSuccess) return e;
+    a.tile_items = units * K::BLOCKS;
     a.g_magic = map_magic_of(a.G);
     a.hk_magic = map_magic_of(a.c.Hk);
-    // a block for every item there can be: a tile for a sequence and for tile_rows more packed rows; pieces are kFewItems and kTileItems
+    // a block for every item there can be: a tile for a sequence and for tile_rows more packed rows; pieces are kFewItems and tile_items
     // more at most (and a few for the rounding of their lengths), fewer where no history is long
     const int64_t tiles = (int64_t)(a.c.S < a.c.T ? a.c.S : a.c.T) + (int64_t)a.c.T * a.G / a.tile_rows;
     const int64_t base = tiles * a.c.Hk;
     const int64_t longest = (int64_t)a.c.max_pages << a.c.page_shift;
     const int64_t by_length = longest > kMinPiece ? base * ((longest - 1) / kMinPiece) : 0;
-    const int64_t most = kFewItems + kTileItems + 64;
-    const int64_t grid = base + (by_length < most ? by_length : most) + 16;      // (either kind's items are dealt out by eights)
+    const int64_t most = kFewItems + a.tile_items + 64;
+    const int64_t grid = base + (by_length < most ? by_length : most) + 16;      // (those of many rows are rounded up to eights)
     if (grid > 0x7fffffff) return hipErrorInvalidValue;
     static bool done[kMaxDevices];
     const auto kern = attention_kernel<T, FP8, DP, EXACT, LIGHT>;
-    const hipError_t e = ensure_lds_limit(kern, K::LDS, done);
+    e = ensure_lds_limit(kern, K::LDS, done);
     if (e != hipSuccess) return e;
     kern<<<(unsigned)grid, 256, K::LDS, s>>>(a);
     return hipGetLastError();

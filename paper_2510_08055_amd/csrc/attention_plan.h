@@ -15,10 +15,13 @@ typedef float float16_t __attribute__((ext_vector_type(16)));
 constexpr float kLowest = -FLT_MAX;      // a running maximum before its first token: finite, so that no difference is NaN
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
-// Items that the pieces of a launch aim at, of each kind of tile.  Pieces are multiples of kMinPiece tokens (a step of 32 for each of
-// a block's four waves), and no shorter than kMinTilePiece where a tile has many rows.
-constexpr int kFewItems = 1024, kTileItems = 512;
-constexpr int kMinPiece = 128, kMinTilePiece = 256;
+// Items that the pieces of a launch aim at: of few rows, kFewItems, and with many rows among them, a round of the blocks that the
+// units hold at once (AttnArgs::tile_items).  Pieces are multiples of kMinPiece tokens (a step of 32 for each of a block's four waves), and no
+// shorter than kMinTilePiece where a tile has many rows: a piece more costs its partial results, 64 KB at dim 128.
+// Measured, us, kFewItems 768 / 1024 / 1536 / 3072: 128 ragged histories 140 / 136 / 138 / 143, 24 drafted ones over FP8 124 / 124 / 120 / 133, 32 short
+// ones 32 / 35 / 35 / 41.  kMinTilePiece 256 / 512 / 768: 300 prompt rows 19 / 17 / 17, 16 drafts of 9 rows over up to 6000 tokens 40 / 31 / 33.
+constexpr int kFewItems = 1024;
+constexpr int kMinPiece = 128, kMinTilePiece = 512;
 
 struct Seq {
     int row0, n, kv;                // first row, rows, tokens held
@@ -122,9 +125,9 @@ __device__ __forceinline__ Item find_item(const AttnArgs& a, int block, PlanShar
     // A token costs an item of either kind about the same time (of a unit's share of the memory, or of its matrix cores).
     auto even = [](float work, int items, int least) {
         const float v = work * (1.0f / (float)items);
-        return v <= (float)least ? least : v < 1e9f ? ((int)v + least) / least * least : 1 << 30;
+        return v <= (float)least ? least : v < 1e9f ? ((int)v + kMinPiece) / kMinPiece * kMinPiece : 1 << 30;
     };
-    int few_piece = even(few, kFewItems, kMinPiece), many_piece = even(few + many, kTileItems, kMinTilePiece);
+    int few_piece = even(few, kFewItems, kMinPiece), many_piece = even(few + many, a.tile_items, kMinTilePiece);
 
     // items of many rows and of few, and units of partial results, of this thread's sequence
     int count[2], need, pieces;
@@ -178,22 +181,10 @@ __device__ __forceinline__ Item find_item(const AttnArgs& a, int block, PlanShar
         if (total[2] <= kPartUnits) break;
         few_piece = many_piece = 1 << 30;      // (more pieces than the workspace holds: none are split)
     }
-    // Of a batch with both kinds of tile, eight blocks take items of many rows and eight of few, in turn and as often as keeps pace with
-    // their numbers: a unit then streams a cache for one block while another one keeps its matrix cores busy.  (Eight at a
-    // time, so that an item's number still decides its XCD.)
-    int kind = total[0] > 0 ? 0 : 1;
-    if (total[0] > 0 && total[1] > 0) {
-        const int groups = (total[0] + 7) / 8, fews = (total[1] + 7) / 8;
-        // of the first g groups of blocks, this many are of many rows
-        const float part = (float)groups / (float)(groups + fews);
-        auto of_many = [&](int g) {
-            const int n = (int)__builtin_ceilf((float)g * part);
-            return n < groups ? n : groups;
-        };
-        const int g = block / 8, before = g < groups + fews ? of_many(g) : groups, until = g + 1 < groups + fews ? of_many(g + 1) : groups;
-        kind = until > before ? 0 : 1;
-        block = (kind == 0 ? before : g - before) * 8 + block % 8;
-    }
+    // Tiles of many rows come first: they take longest.  (As many blocks as eights of them, so that an item's number still decides its
+    // XCD.  512 prompt rows over 7680 tokens beside 32 decode rows, us: this order 117, decode rows first 121, both in turn 139.)
+    const int first = (total[0] + 7) / 8 * 8, kind = block < first ? 0 : 1;
+    if (kind == 1) block -= first;
     if (block >= total[kind]) return it;
     int rem = 0, pc = 1;
     auto found = [&](int b, int slots, auto put) {
@@ -234,12 +225,12 @@ __device__ __forceinline__ Item find_item(const AttnArgs& a, int block, PlanShar
         it.seq = get(5); rem = get(6); pc = get(7); it.slot = get(8);
     }
     it.q.many = kind == 0;
-    // heads side by side (they go to different XCDs, and the tiles of a head to the same ones), long tiles first
+    // Heads side by side, then tiles, long ones first, then pieces.  (Consecutive blocks go to the XCDs in turn: a head's tiles meet on
+    // few of them, and no XCD is left with the last pieces, which short tiles do not have.)
     const int across = Hk == 1 ? rem : (int)divided((uint32_t)rem, (uint32_t)Hk, a.hk_magic);
     it.head = rem - across * Hk;
-    const int down = pc == 1 ? across : across / pc;
-    it.sub = across - down * pc;
-    it.tile = it.q.tiles - 1 - down;
+    it.sub = pc == 1 ? 0 : across / it.q.tiles;
+    it.tile = it.q.tiles - 1 - (across - it.sub * it.q.tiles);
     it.piece = pc == 1 ? 0 : it.q.many ? many_piece : few_piece;
     it.slot += (it.tile * Hk + it.head) * pc * it.q.units;
     it.valid = true;
@@ -409,7 +400,7 @@ template <typename T, int DP, int UNITS>
 __device__ __forceinline__ void join_pieces(const AttnArgs& a, const Item& it, const Range& rg, int D, int32_t* flag)
 {
     if (!last_to_arrive(a.tickets + it.slot, (uint32_t)rg.pieces, flag)) return;
-    constexpr int ND = (DP + 63) / 64, AT_ONCE = UNITS > 1 && ND <= 2 ? 2 : 1;      // units
+    constexpr int ND = (DP + 63) / 64, AT_ONCE = UNITS == 1 || ND == 4 ? 1 : 4 / ND < UNITS ? 4 / ND : UNITS;      // units, as many as 64 registers hold
     const int units = it.q.units, d0 = (threadIdx.x & 15) * 4, q = threadIdx.x >> 4;
     const Parts parts = parts_of(a, D);
     for (int u0 = 0; u0 < units; u0 += AT_ONCE) {
@@ -427,20 +418,23 @@ __device__ __forceinline__ void join_pieces(const AttnArgs& a, const Item& it, c
             float2 st[4][AT_ONCE];
             float4 x[4][AT_ONCE][ND];
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < 4; ++c) {
+                if (c0 + c < rg.pieces) {
 #pragma unroll
-                for (int u = 0; u < AT_ONCE; ++u) {
-                    const int at = c0 + c < rg.pieces ? c0 + c : rg.pieces - 1;
-                    const int row = (it.slot + at * units + u0 + u) * 16 + q;
-                    st[c][u] = load_part_stats(a, row);
+                    for (int u = 0; u < AT_ONCE; ++u) {
+                        const int row = (it.slot + (c0 + c) * units + u0 + u) * 16 + q;
+                        st[c][u] = load_part_stats(a, row);
 #pragma unroll
-                    for (int k = 0; k < ND; ++k) x[c][u][k] = load_part(parts, row, d0 + k * 64 < D ? d0 + k * 64 : 0);
+                        for (int k = 0; k < ND; ++k) x[c][u][k] = load_part(parts, row, d0 + k * 64 < D ? d0 + k * 64 : 0);
+                    }
                 }
+            }
 #pragma unroll
             for (int u = 0; u < AT_ONCE; ++u) {
                 float top = M[u];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) top = fmaxf(top, st[c][u].x);
+                for (int c = 0; c < 4; ++c)
+                    if (c0 + c < rg.pieces) top = fmaxf(top, st[c][u].x);
                 const float back = __builtin_amdgcn_exp2f(M[u] - top);
                 M[u] = top;
                 L[u] *= back;

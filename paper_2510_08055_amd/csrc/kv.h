@@ -42,6 +42,7 @@ struct AttnArgs {
     int Hq, G, causal, window;
     int few_rows, tile_rows;       // packed rows of a tile, up to few_rows and where a sequence has more (set by the launch, as are:)
     int tile_tokens;               // tile_rows / G
+    int tile_items;                // items that a batch with tiles of many rows is cut into
     uint32_t g_magic, hk_magic;    // for divisions by G and by Hk
     float scale2;                  // log2(e) / sqrt(dim): scores are kept as powers of two
     float* part;                   // partial outputs, kPartUnits of 16 rows x D
