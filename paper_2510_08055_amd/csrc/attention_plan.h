@@ -18,9 +18,12 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 // Items that the pieces of a launch aim at: of few rows, kFewItems, and with many rows among them, a round of the blocks that the
 // units hold at once (AttnArgs::tile_items).  Pieces are multiples of kMinPiece tokens (a step of 32 for each of a block's four waves), and no
 // shorter than kMinTilePiece where a tile has many rows: a piece more costs its partial results, 64 KB at dim 128.
-// Measured, us, kFewItems 768 / 1024 / 1536 / 3072: 128 ragged histories 140 / 136 / 138 / 143, 24 drafted ones over FP8 124 / 124 / 120 / 133, 32 short
-// ones 32 / 35 / 35 / 41.  kMinTilePiece 256 / 512 / 768: 300 prompt rows 19 / 17 / 17, 16 drafts of 9 rows over up to 6000 tokens 40 / 31 / 33.
-constexpr int kFewItems = 1024;
+// Measured, us, kFewItems 384 / 512 / 1024 / 2048: 128 ragged histories of up to 8192 tokens 152 / 139 / 136 / 139, 24 drafted ones over FP8 106 / 120 /
+// 120 / 125 (how the last pieces fall), 32 of up to 4096 tokens 31 / 29 / 35 / 41, 128 of up to 1024 29 / 27 / 29 / 34.  (Equal stretches of all the
+// work laid end to end, one to a block, bring the first two to 127 and 104, but their longer plan costs every launch 2 us, and the
+// others 20 to 40 %.)
+// kMinTilePiece 256 / 512 / 768: 300 prompt rows 19 / 17 / 17, 16 drafts of 9 rows over up to 6000 tokens 40 / 31 / 33.
+constexpr int kFewItems = 512;
 constexpr int kMinPiece = 128, kMinTilePiece = 512;
 
 struct Seq {
