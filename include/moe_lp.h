@@ -312,7 +312,9 @@ moe_status moe_set_ffn_variant(moe_ctx *ctx, int32_t variant);
  * A token whose table entry is not in [0, n_pages), or lies beyond max_pages, is not there: nothing is written for it, nothing sees
  * it, and it reads back as zeros.  Entries of pages that a sliding window has left behind are set to -1 that way.  (Where a position
  * is negative, because kv_lens[s] is less than the sequence's rows, the row is not written, and sees nothing under a causal mask.)
- * Descriptors live on the device and are read by every call, so a captured graph replays with what they then hold.
+ * Descriptors live on the device and are read by every call, so a captured graph replays with what they then hold.  Row offsets that
+ * descend or leave [0, T] make moe_paged_attention compute nothing; no descriptor makes a call touch memory outside its tensors.
+ * Limits (MOE_ERR_SHAPE): T * heads <= 2^30, max_pages * page <= 2^30, n_seqs < 2^22, n_pages < 2^31.
  */
 typedef enum { MOE_KV_DTYPE = 0, MOE_KV_FP8 = 1 } moe_kv_format;
 

@@ -53,13 +53,13 @@ moe_status view_of(const moe_kv_ctx* ctx, const moe_kv_pages* pages, const moe_k
     if (!pages || !batch) return MOE_ERR_NULL;
     const moe_kv_config& g = ctx->cfg;
     if (T < 0 || batch->n_seqs < 0 || batch->max_pages < 0) return MOE_ERR_SHAPE;
-    if (T * (int64_t)g.heads > kMaxInt / 64 || T > kMaxInt / 64) return MOE_ERR_SHAPE;      // rows of heads are counted in 32 bits
+    if (T > ((int64_t)1 << 30) / g.heads) return MOE_ERR_SHAPE;      // rows of heads are counted in 32 bits
     if (T > 0) {
         if (!pages->k_pages || !pages->v_pages || !batch->row_offsets || !batch->kv_lens) return MOE_ERR_NULL;
         if (batch->max_pages > 0 && !batch->page_table) return MOE_ERR_NULL;
         if (g.kv_format == MOE_KV_FP8 && (!pages->k_scales || !pages->v_scales)) return MOE_ERR_NULL;
         if (pages->n_pages < 1 || pages->n_pages > kMaxInt || batch->n_seqs < 1 || batch->n_seqs > kMaxInt / 512 ||
-            batch->max_pages * (int64_t)g.page > kMaxInt / 2)
+            batch->max_pages > ((int64_t)1 << 30) / g.page)
             return MOE_ERR_SHAPE;
         if (misaligned(pages->k_pages) || misaligned(pages->v_pages) || misaligned(pages->k_scales) || misaligned(pages->v_scales))
             return MOE_ERR_ALIGN;

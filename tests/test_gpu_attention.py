@@ -246,3 +246,39 @@ def test_replays_of_a_graph_take_the_descriptors_as_they_are(gpu_lib):
             assert torch.equal(got, want), f"replay {rep}"
         ref, _, tol, _ = b.reference()
         assert_within(out, ref, tol, f"replay {rep}")
+
+
+@pytest.mark.parametrize("n_seqs", [50, 200, 400])
+def test_prompts_among_many_sequences(gpu_lib, n_seqs):
+    rows = [[1, 0, 2, 1][s % 4] for s in range(n_seqs)]
+    kv = [max(n, (s * 29) % 150) for s, n in enumerate(rows)]
+    for s, n, k in ((3, 90, 700), (n_seqs - 2, 300, 300), (n_seqs // 2, 17, 2500)):
+        rows[s], kv[s] = n, k
+    check(gpu_lib, Batch(rows, kv, 16, 2, 64, 16, seed=n_seqs), sinks=sinks_of(16))
+
+
+@pytest.mark.parametrize("dim", [64, 80, 128, 256])
+@pytest.mark.parametrize("dtype,fmt", [(torch.bfloat16, ""), (torch.bfloat16, "fp8"), (torch.float32, "")])
+def test_long_histories_in_several_pieces(gpu_lib, dim, dtype, fmt):
+    check(gpu_lib, Batch([70, 3, 1, 20], [4100, 3000, 5000, 1700], 8, 2, dim, 32, dtype, fmt, seed=dim), sinks=sinks_of(8))
+    check(gpu_lib, Batch([150], [3333], 4, 2, dim, 8, dtype, fmt, seed=dim + 1), window=1500)
+
+
+def test_a_first_call_may_be_captured(gpu_lib):
+    """What a context clears once belongs to the graph then, and eager calls before and between its replays find it cleared too."""
+    b = Batch([1, 40], [3000, 2000], 8, 2, 64, 16, seed=43)
+    ref, _, tol, _ = b.reference()
+    ctx, pages, batch = b.context(gpu_lib)
+    ctx.workspace.fill_(0xff)
+    out = torch.zeros(b.T, 8, 64, dtype=torch.bfloat16, device=DEV)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.moe_paged_attention(b.q, pages, batch, out=out)
+    for _ in range(3):
+        assert_within(ctx.moe_paged_attention(b.q, pages, batch), ref, tol, "eager")
+        torch.cuda.synchronize()
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert_within(out, ref, tol, "replay")

@@ -105,6 +105,11 @@ def test_many_sequences(gpu_lib, n_seqs):
     check_append(gpu_lib, Batch(rows, kv, 1, 1, 16, 8, seed=n_seqs))
 
 
+def test_many_empty_sequences_between_two_rows(gpu_lib):
+    rows = [1] + [0] * 70 + [2] + [0] * 200 + [1, 0, 3]
+    check_append(gpu_lib, Batch(rows, [n + 3 for n in rows], 2, 2, 64, 8, seed=3))
+
+
 def test_pages_far_into_a_cache(gpu_lib):
     # rows past 2^32 bytes of the pages
     n_pages, page, kv_heads, dim = 150000, 16, 8, 128
