@@ -15,12 +15,19 @@ namespace {
 // the transposing reads (a lane gets one dimension of four tokens), in the token order that the exponentials happen to have.
 // A row of 256 bytes would put the same dimensions of every token on the same banks; its 16-byte chunks are permuted, chunk c of
 // token t in place c ^ swz(t), so that both kinds of read touch every bank equally.
+//
+// Why 128 rows and four waves: a step's 32 KB of operands are read from LDS by every wave for its 32 rows, 128 bytes a cycle if the matrix
+// pipes never paused, and two such blocks share a unit, each with its own barrier, so that one's exponentials run beside the other's
+// products.  What bounds it at dim 128: the matrix pipes at the clock that they leave (2.0 GHz), busy 46 % of a causal prompt of 8192 tokens and 32
+// heads (580 us with 128 decode rows, 0.95 PFLOP/s), half of all steps' issue being vector instructions.  8192 rows to 8192 tokens, no
+// mask, 32 heads: dim 128 1043 us (1.05 PFLOP/s), FP8 pages 1139; dim 64 628 (0.88: as many exponentials for half the products), FP8 666; 4096 to 4096,
+// 16 heads, dim 256, one block to a unit: 420 (0.65).
 // ----------------------------------------------------------------------------------------------------------------
 constexpr int kManyRows = 128;
 
 // N direct-to-LDS loads of a wave, 1 KB after the other in LDS and, but for what the offsets make good, in memory (the
 // instruction's offset counts in both): M0 is written once for all of them.
-constexpr uint32_t kGroupBias = 3072;        // keeps the 32-bit offsets from falling below zero
+constexpr uint32_t kGroupBias = 3 * 1024;    // keeps the 32-bit offsets from falling below zero
 template <int N> __device__ __forceinline__ void load_lds_group(const uint32_t (&off)[N], const char* base, uint32_t lds)
 {
     if constexpr (N == 1)
@@ -30,8 +37,8 @@ template <int N> __device__ __forceinline__ void load_lds_group(const uint32_t (
                      "v"(off[1]), "s"(base), "s"(lds) : "memory");
     else
         asm volatile("s_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024\n\t"
-                     "global_load_lds_dwordx4 %2, %4 offset:2048\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072" ::"v"(off[0]), "v"(off[1]),
-                     "v"(off[2]), "v"(off[3]), "s"(base), "s"(lds) : "memory");
+                     "global_load_lds_dwordx4 %2, %4 offset:2048\n\tglobal_load_lds_dwordx4 %3, %4 offset:%6" ::"v"(off[0]), "v"(off[1]),
+                     "v"(off[2]), "v"(off[3]), "s"(base), "s"(lds), "n"(kGroupBias) : "memory");
 }
 
 template <bool FP8, int DP, bool EXACT> struct Many {
@@ -306,7 +313,7 @@ template <bool FP8, int DP, bool EXACT> struct Many {
                         const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k / 2][(k % 2) * 8 + 2 * i + 1], a.scale2, -m));
                         l += p0;
                         l += p1;
-                        u[i] = pack_bf16x2(p0, p1);
+                        u[i] = pack_bf16x2(p0, p1);      // (see Few::weights_of)
                     }
                     w[k] = __builtin_bit_cast(bf16x8_t, make_uint4(u[0], u[1], u[2], u[3]));
                 }
