@@ -310,7 +310,8 @@ moe_status moe_set_ffn_variant(moe_ctx *ctx, int32_t variant);
  * kv_lens[s] tokens, of which they are the last: row i of n stands at position kv_lens[s] - n + i.  Token j lies in slot
  * j % page of page page_table[s, j / page] (page_table [n_seqs, max_pages] int32).
  * A token whose table entry is not in [0, n_pages), or lies beyond max_pages, is not there: nothing is written for it, nothing sees
- * it, and it reads back as zeros.  Entries of pages that a sliding window has left behind are set to -1 that way.  (Where a position
+ * it, and it reads back as zeros.  Entries of pages that a sliding window has left behind are set to -1 that way.  The positions of the
+ * rows, and with them what a causal mask or a window shows, are those of kv_lens[s] whether or not the table reaches them.  (Where a position
  * is negative, because kv_lens[s] is less than the sequence's rows, the row is not written, and sees nothing under a causal mask.)
  * Descriptors live on the device and are read by every call, so a captured graph replays with what they then hold.  Row offsets that
  * descend or leave [0, T] make moe_paged_attention compute nothing; no descriptor makes a call touch memory outside its tensors.

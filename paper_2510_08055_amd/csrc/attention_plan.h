@@ -27,7 +27,7 @@ constexpr int kFewItems = 512;
 constexpr int kMinPiece = 128, kMinTilePiece = 512;
 
 struct Seq {
-    int row0, n, kv;                // first row, rows, tokens held
+    int row0, n, kv;                // first row, rows, tokens with them (of which the table need not reach all: held_of)
     int tiles, units, len;          // tiles of packed rows, units of 16 rows to a tile, tokens of the longest tile's range
     bool many;                      // its tiles are those of attention_tile.h
 };
@@ -39,25 +39,31 @@ struct Item {
     bool valid;
 };
 
+// The tokens of a sequence that can be there, those its row of the table reaches.  Positions are taken from its length as it is.
+__device__ __forceinline__ int held_of(const KVView& c, int kv)
+{
+    const int most = c.max_pages << c.page_shift;
+    return kv < most ? kv : most;
+}
+
 __device__ __forceinline__ Seq shape_of(const AttnArgs& a, int lo, int hi, int kv)
 {
     Seq q;
-    const int most = a.c.max_pages << a.c.page_shift;
     q.row0 = lo;
     q.n = hi - lo;
-    q.kv = kv < 0 ? 0 : (kv > most ? most : kv);
+    q.kv = kv < 0 ? 0 : kv;
     const int rows = q.n * a.G;
     q.many = rows > a.few_rows && a.tile_rows > a.few_rows;
     const int per = rows <= 16 ? 16 : rows <= a.few_rows ? a.few_rows : a.tile_rows;      // (all powers of two)
     q.units = per / 16;
     q.tiles = (rows + per - 1) >> (31 - __builtin_clz(per));
-    q.len = q.kv;
-    if (a.window > 0) {
+    q.len = held_of(a.c, q.kv);
+    if (a.window > 0) {                                      // (windows, rows and what the table reaches are at most 2^30)
         const int first = q.kv - q.n - a.window + 1;
-        int len = q.kv - (first > 0 ? first : 0) + 31;
-        const int one = a.window + a.tile_tokens + 2 + 31;   // (windows are at most 2^30)
+        int len = q.len - (first > 0 ? first : 0) + 31;
+        const int one = a.window + a.tile_tokens + 2 + 31;
         if (a.causal && one < len) len = one;
-        if (len < q.len) q.len = len;
+        if (len < q.len) q.len = len > 0 ? len : 0;
     }
     return q;
 }
@@ -249,6 +255,7 @@ __device__ __forceinline__ int token_of(const AttnArgs& a, int r)
 // The tokens that a tile's rows see: all rows those of [full_lo, full_hi), some row those of [lo, hi); lo is a multiple of 32.
 struct Range {
     int p0;                         // position of the sequence's first row
+    int held;                       // tokens of the sequence that can be there
     int rows, first;                // packed rows of the sequence, the tile's first
     int lo, hi, full_lo, full_hi;
     int pieces;
@@ -262,10 +269,11 @@ __device__ __forceinline__ Range range_of(const AttnArgs& a, const Item& it)
     const int end = r.first + it.q.units * 16;
     const int last = (end < r.rows ? end : r.rows) - 1;
     r.p0 = it.q.kv - it.q.n;
+    r.held = held_of(a.c, it.q.kv);
     const int p_first = r.p0 + token_of(a, r.first), p_last = r.p0 + token_of(a, last);
-    r.hi = a.causal && p_last + 1 < it.q.kv ? p_last + 1 : it.q.kv;
+    r.hi = a.causal && p_last + 1 < r.held ? p_last + 1 : r.held;
     if (r.hi < 0) r.hi = 0;
-    r.full_hi = a.causal && p_first + 1 < it.q.kv ? p_first + 1 : it.q.kv;
+    r.full_hi = a.causal && p_first + 1 < r.held ? p_first + 1 : r.held;
     r.lo = a.window > 0 && p_first - a.window + 1 > 0 ? p_first - a.window + 1 : 0;
     r.full_lo = a.window > 0 && p_last - a.window + 1 > 0 ? p_last - a.window + 1 : 0;
     r.lo &= ~31;
@@ -297,7 +305,7 @@ __device__ __forceinline__ Row row_of(const AttnArgs& a, const Item& it, const R
     x.row = it.q.row0 + tok;
     x.head = it.head * a.G + (x.there ? r - tok * a.G : 0);
     const int p = rg.p0 + tok;
-    x.see_hi = !x.there ? 0 : (a.causal && p + 1 < it.q.kv ? p + 1 : it.q.kv);
+    x.see_hi = !x.there ? 0 : (a.causal && p + 1 < rg.held ? p + 1 : rg.held);
     x.see_lo = a.window > 0 ? p - a.window + 1 : 0;
     return x;
 }

@@ -1,0 +1,72 @@
+"""Attention over a paged cache where descriptors and contents are at their edges, against the definition in 64 bits (bounds as in
+test_gpu_attention.py)."""
+import math
+
+import pytest
+import torch
+
+from kv_reference import Batch, assert_within, attention
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+FORMS = [(torch.bfloat16, ""), (torch.bfloat16, "fp8"), (torch.float32, ""), (torch.float32, "fp8")]
+
+
+def sinks_of(heads, seed=3):
+    return torch.randn(heads, generator=torch.Generator().manual_seed(seed)).to(DEV)
+
+
+def call(lib, b, **options):
+    ctx, pages, batch = b.context(lib)
+    lse = torch.full((b.T, b.heads), 7.0, device=DEV)
+    out = ctx.moe_paged_attention(b.q, pages, batch, lse=lse, **options)
+    return out, lse
+
+
+def check(lib, b, causal=True, window=0, sinks=None):
+    """The reference takes positions from its lengths only where its table reaches that far: entries of -1 take the table there."""
+    wide = torch.full((len(b.kv), max(-(-k // b.page) for k in b.kv) + 1), -1, dtype=torch.int32, device=DEV)
+    n = min(wide.shape[1], b.table.shape[1])
+    wide[:, :n] = b.table[:, :n]
+    out, lse = call(lib, b, causal=causal, window=window, sinks=sinks)
+    ref, ref_lse, tol, ltol = attention(b.q, b.pages(), b.offsets, b.kv, wide, b.page, causal, window, sinks)
+    tol = torch.where(ref.isnan(), 0.0, tol)      # (where the result has no finite value only that is asked for)
+    assert_within(out, ref, tol, "out")
+    assert_within(lse, ref_lse, ltol, "lse")
+    return out, lse
+
+
+# ---- lengths past the table: the rows keep their positions, the tokens that the table does not reach are not there ----
+
+def short_table(rows, kv, columns, heads, kv_heads, dim, page, dtype, fmt, seed):
+    b = Batch(rows, kv, heads, kv_heads, dim, page, dtype, fmt, seed=seed)
+    b.table = b.table[:, :columns].contiguous()
+    return b
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("window", [0, 5, 40, 2 ** 29])
+@pytest.mark.parametrize("dtype,fmt", FORMS)
+def test_lengths_past_the_table(gpu_lib, dtype, fmt, window, causal):
+    # two pages of eight: positions 12 to 19 and 0 to 39, of which tokens 0 to 15 are there; decode rows inside and far behind
+    check(gpu_lib, short_table([8, 40, 1, 1, 3], [20, 40, 16, 200, 9], 2, 4, 2, 64, 8, dtype, fmt, 3), causal, window)
+    # decode rows alone; rows for tiles of 32 and of 128
+    check(gpu_lib, short_table([1, 1, 1], [70, 64, 50], 4, 8, 1, 128, 16, dtype, fmt, 5), causal, window, sinks_of(8))
+    check(gpu_lib, short_table([30, 150, 150], [90, 150, 400], 5, 1, 1, 64, 16, dtype, fmt, 7), causal, window)
+    # histories in several pieces
+    check(gpu_lib, short_table([2, 140], [6000, 5000], 250, 2, 2, 64, 16, dtype, fmt, 9), causal, window)
+
+
+@pytest.mark.parametrize("dtype,fmt", FORMS)
+@pytest.mark.parametrize("rows", [1, 20, 150])
+def test_the_longest_lengths(gpu_lib, rows, dtype, fmt):
+    b = Batch([rows, 1], [160, 30], 4, 2, 64, 16, dtype, fmt, seed=rows)
+    want, want_lse = call(gpu_lib, b, causal=False)
+    b.kv_lens[0] = 2 ** 31 - 1                # every token that the table holds is behind the rows
+    for causal in (True, False):
+        out, lse = call(gpu_lib, b, causal=causal)
+        assert torch.equal(out[:rows], want[:rows]) and torch.equal(lse[:rows], want_lse[:rows])
+        for window in (1, 50, 2 ** 30):
+            out, lse = call(gpu_lib, b, causal=causal, window=window)
+            assert (out[:rows] == 0).all() and (lse[:rows] == -math.inf).all()
+            assert torch.isfinite(out.float()).all()
