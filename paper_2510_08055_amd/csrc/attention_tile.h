@@ -296,8 +296,10 @@ template <bool FP8, int DP, bool EXACT> struct Many {
                     for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
                 top = swap_max(top) * a.scale2;                      // (the scale is positive)
                 // (the reference of the exponentials follows the maximum only when that has grown by more than 8, see attention_few.h)
+                // Before a row's first token there is nothing to scale but what clean_values gave it in this step, which no factor may touch:
+                // zero times an infinity would be NaN.
                 if (__any(top > m + 8.0f)) {
-                    const float to = fmaxf(top, m), f = __builtin_amdgcn_exp2f(m - to);
+                    const float to = fmaxf(top, m), f = m == kLowest ? 1.0f : __builtin_amdgcn_exp2f(m - to);
                     m = to;
                     l *= f;
 #pragma unroll

@@ -70,3 +70,24 @@ def test_the_longest_lengths(gpu_lib, rows, dtype, fmt):
             out, lse = call(gpu_lib, b, causal=causal, window=window)
             assert (out[:rows] == 0).all() and (lse[:rows] == -math.inf).all()
             assert torch.isfinite(out.float()).all()
+
+
+# ---- values that are not finite, where a row first sees anything ----
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("rows,kv,window,at", [(150, 150, 0, 10), (150, 150, 0, 0), (150, 1000, 200, 700), (150, 1000, 70, 900), (40, 40, 0, 10),
+                                               (20, 20, 0, 10), (1, 90, 20, 75)])
+@pytest.mark.parametrize("dtype,dim,group", [(torch.bfloat16, 64, 1), (torch.bfloat16, 128, 8), (torch.bfloat16, 256, 1), (torch.bfloat16, 80, 2),
+                                             (torch.float32, 64, 1)])
+def test_strange_values_in_a_first_step(gpu_lib, dtype, dim, group, rows, kv, window, at, bad):
+    b = Batch([rows], [kv], group, 1, dim, 16, dtype, seed=13)
+    b.v_pages[int(b.table[0, at // 16]), 0, at % 16, 5] = bad
+    out, lse = check(gpu_lib, b, window=window)
+    pos = torch.arange(kv - rows, kv, device=DEV)
+    sees = (pos >= at) & ((pos - at < window) if window else torch.ones_like(pos, dtype=torch.bool))
+    assert sees.any()
+    got = out[sees][..., 5].float()
+    assert torch.equal(got.nan_to_num(123.0, 1e30, -1e30), torch.full_like(got, bad).nan_to_num(123.0, 1e30, -1e30))
+    assert torch.isfinite(out[~sees].float()).all() and torch.isfinite(lse).all()
+    others = [d for d in range(dim) if d != 5]
+    assert torch.isfinite(out[..., others].float()).all()
