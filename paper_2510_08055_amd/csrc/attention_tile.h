@@ -156,7 +156,7 @@ template <bool FP8, int DP, bool EXACT> struct Many {
             for (int g = 0; g < 2; ++g)
 #pragma unroll
                 for (int i = 0; i < GL; ++i) {
-                    // (chunks past the dimension: keys meet zeros there, values go to outputs that are not stored)
+                    // (chunks past the dimension: no product reads those of the keys, those of the values go to outputs that are not stored)
                     const int chunk = c ^ swz(g * 8 + i * TPL + tl);
                     from[g][i] = (uint32_t)((i * TPL + tl) * D * 2 + (chunk * 8 < D ? chunk * 16 : 0) - i * 1024) + kGroupBias;
                 }
@@ -274,11 +274,18 @@ template <bool FP8, int DP, bool EXACT> struct Many {
             if (!idle) {
                 float16_t s[2];
 #pragma unroll
-                for (int c = 0; c < DP / 16; ++c)
+                for (int c = 0; c < DP / 16; ++c) {
+                    // Past the dimension: what is staged there is no key, and an infinity of it would be NaN against a query of zeros.  Its products
+                    // are left out, at 256 its chunks are made zeros (3000 rows to 3000 tokens, 32 heads, us, products of it all / left out / zeros: dim 80
+                    // 95 / 88 / -, 112 94 / 89 / -, 208 273 / 381 / 280: with one wave to a SIMD nothing hides the reads of a loop in pieces).
+                    if (!EXACT && DP <= 128 && c * 16 >= D) break;
 #pragma unroll
-                    for (int b = 0; b < 2; ++b)
-                        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_keys(k_at[c] + b * 32 * ROWB), qf[c], c == 0 ? float16_t{} : s[b],
-                                                                       0, 0, 0);
+                    for (int b = 0; b < 2; ++b) {
+                        bf16x8_t key = read_keys(k_at[c] + b * 32 * ROWB);
+                        if (!EXACT && DP > 128 && c * 16 >= DP / 2 && c * 16 >= D) key = bf16x8_t{};
+                        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key, qf[c], c == 0 ? float16_t{} : s[b], 0, 0, 0);
+                    }
+                }
                 if (masked) {
 #pragma unroll
                     for (int b = 0; b < 2; ++b)

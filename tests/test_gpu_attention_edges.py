@@ -91,3 +91,17 @@ def test_strange_values_in_a_first_step(gpu_lib, dtype, dim, group, rows, kv, wi
     assert torch.isfinite(out[~sees].float()).all() and torch.isfinite(lse).all()
     others = [d for d in range(dim) if d != 5]
     assert torch.isfinite(out[..., others].float()).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,group", [(1, 4), (4, 8), (30, 1), (150, 1)])
+@pytest.mark.parametrize("dim", [16, 48, 64, 80, 96, 112, 128, 144, 208, 256])
+def test_keys_of_minus_infinity_are_weights_of_zero(gpu_lib, dim, rows, group, dtype):
+    """At every width, in the first dimensions too: a score of minus infinity, not NaN."""
+    kv = rows + 100
+    b = Batch([rows], [kv], group, 1, dim, 16, dtype, seed=dim)
+    b.q[..., 3] = b.q[..., 3].abs() + 0.125
+    for at in (20, kv - rows + rows // 2):
+        b.k_pages[int(b.table[0, at // 16]), 0, at % 16, 3] = -math.inf
+    out, lse = check(gpu_lib, b)
+    assert torch.isfinite(out.float()).all() and torch.isfinite(lse).all()
