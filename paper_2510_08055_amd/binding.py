@@ -368,20 +368,23 @@ def kv_workspace_bytes(heads, kv_heads, dim, page, dtype, kv_format="") -> int:
 
 
 class KVPages(CKVPages):
-    """The pages of one layer (moe_kv_pages); keeps their tensors alive."""
+    """The pages of one layer (moe_kv_pages); keeps their tensors alive, and the layout that they were checked for."""
     tensors = ()
+    layout = None
 
 
 class KVBatch(CKVBatch):
     """A batch's descriptors (moe_kv_batch); keeps their tensors alive."""
     tensors = ()
+    device = None
 
 
 class KVContext:
     """A moe_kv_ctx plus the torch-allocated workspace it lives on: a paged key/value cache's format and its attention.
 
     Tensors of rows (q, k, v and what comes back) are [T, heads, dim] with any stride between rows, so views of one fused
-    projection can be handed over.  The struct of a batch holds pointers only: what its tensors hold when a call runs counts."""
+    projection can be handed over.  The struct of a batch holds pointers only: what its tensors hold when a call runs counts.
+    Contexts of the same layout (kv_heads, page, dim, the pages' type, the GPU) may share packed pages; others refuse them."""
 
     def __init__(self, heads, kv_heads, dim, page, dtype=torch.bfloat16, kv_format="", device="cuda:0"):
         self.lib = load()
@@ -395,6 +398,7 @@ class KVContext:
         n = ctypes.c_size_t(0)
         _check(self.lib.moe_kv_workspace_bytes(ctypes.byref(self.cfg), ctypes.byref(n)), "moe_kv_workspace_bytes")
         self.workspace = torch.empty(n.value + 256, dtype=torch.uint8, device=self.device)
+        self.layout = (kv_heads, page, dim, self.page_dtype, self.workspace.device)
         base = (self.workspace.data_ptr() + 255) // 256 * 256
         self._ctx = ctypes.c_void_p()
         _check(self.lib.moe_kv_create(ctypes.byref(self.cfg), ctypes.c_void_p(base), n.value, ctypes.byref(self._ctx)), "moe_kv_create")
@@ -420,6 +424,13 @@ class KVContext:
                 return self._call(name, *args)
         # (the handle itself: torch.cuda.current_stream() takes 3 us to wrap it, as long as a launch)
         _check(getattr(self.lib, name)(self._ctx, *args, torch._C._cuda_getCurrentRawStream(gpu)), name)
+
+    def _packed(self, pages, batch):
+        """The structs hold pointers alone, so what pack_pages and pack_batch checked has to be what this context reads."""
+        if getattr(pages, "layout", None) != self.layout:
+            raise ValueError(f"pages packed for {getattr(pages, 'layout', None)} do not belong to a context of {self.layout}")
+        if getattr(batch, "device", None) != self.workspace.device:
+            raise ValueError(f"a batch packed on {getattr(batch, 'device', None)} does not belong to a context on {self.workspace.device}")
 
     def _dense(self, t, name, dtype, shape):
         if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != self.workspace.device:
@@ -451,6 +462,7 @@ class KVContext:
         elif k_scales is not None or v_scales is not None:
             raise ValueError("scales belong to FP8 pages")
         p.tensors = (k_pages, v_pages, k_scales, v_scales)
+        p.layout = self.layout
         return p
 
     def pack_batch(self, row_offsets, kv_lens, page_table) -> KVBatch:
@@ -459,11 +471,13 @@ class KVContext:
         b = KVBatch(self._dense(row_offsets, "row_offsets", torch.int32, (n + 1,)), self._dense(kv_lens, "kv_lens", torch.int32, (n,)),
                     self._dense(page_table, "page_table", torch.int32, (n, page_table.shape[1])), n, page_table.shape[1])
         b.tensors = (row_offsets, kv_lens, page_table)
+        b.device = self.workspace.device
         return b
 
     # ---- the calls of the boundary, same names as the C ABI ----
 
     def moe_kv_append(self, k, v, pages, batch):
+        self._packed(pages, batch)
         T = k.shape[0]
         kp, ldk = self._rows(k, "k", T, self.kv_heads)
         vp, ldv = self._rows(v, "v", T, self.kv_heads)
@@ -471,6 +485,7 @@ class KVContext:
 
     def moe_kv_gather(self, pages, batch, T=None, k=None, v=None):
         """The rows' keys and values [T, kv_heads, dim]; T: the batch's rows, needed where no outputs are passed in."""
+        self._packed(pages, batch)
         if k is None or v is None:
             T = T if T is not None else (k if k is not None else v).shape[0]
             made = [torch.empty((T, self.kv_heads, self.dim), dtype=self.dtype, device=self.device) for t in (k, v) if t is None]
@@ -484,6 +499,7 @@ class KVContext:
 
     def moe_paged_attention(self, q, pages, batch, causal=True, window=0, sinks=None, out=None, lse=None):
         """out [T, heads, dim]; lse: a [T, heads] fp32 tensor to receive the rows' log-sum-exp, or None."""
+        self._packed(pages, batch)
         T = q.shape[0]
         if out is None:
             out = torch.empty((T, self.heads, self.dim), dtype=self.dtype, device=self.device)
