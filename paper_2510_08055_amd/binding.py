@@ -360,8 +360,20 @@ class Context:
         _check(self.lib.moe_set_ffn_variant(self._ctx, v), "moe_set_ffn_variant")
 
 
+def _int32(**sizes):
+    """The sizes in their order; ctypes would drop their upper bits without a word."""
+    for name, v in sizes.items():
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise ValueError(f"{name}: {v} does not fit 32 bits")
+    return [int(v) for v in sizes.values()]
+
+
+def _kv_config(heads, kv_heads, dim, page, dtype, kv_format):
+    return CKVConfig(*_int32(heads=heads, kv_heads=kv_heads, dim=dim, page=page), _dtype_code(dtype), KV_FORMATS[kv_format])
+
+
 def kv_workspace_bytes(heads, kv_heads, dim, page, dtype, kv_format="") -> int:
-    cfg = CKVConfig(heads, kv_heads, dim, page, _dtype_code(dtype), KV_FORMATS[kv_format])
+    cfg = _kv_config(heads, kv_heads, dim, page, dtype, kv_format)
     out = ctypes.c_size_t(0)
     _check(load().moe_kv_workspace_bytes(ctypes.byref(cfg), ctypes.byref(out)), "moe_kv_workspace_bytes")
     return out.value
@@ -392,7 +404,7 @@ class KVContext:
         self.dtype = dtype
         self.kv_format = kv_format
         self.device = torch.device(device)
-        self.cfg = CKVConfig(heads, kv_heads, dim, page, _dtype_code(dtype), KV_FORMATS[kv_format])
+        self.cfg = _kv_config(heads, kv_heads, dim, page, dtype, kv_format)
         self.fp8 = self.cfg.kv_format == MOE_KV_FP8
         self.page_dtype = torch.float8_e4m3fn if self.fp8 else dtype
         n = ctypes.c_size_t(0)
@@ -505,7 +517,7 @@ class KVContext:
             out = torch.empty((T, self.heads, self.dim), dtype=self.dtype, device=self.device)
         qp, ldq = self._rows(q, "q", T, self.heads)
         op, ldo = self._rows(out, "out", T, self.heads)
-        opt = CAttentionOptions(int(bool(causal)), int(window),
+        opt = CAttentionOptions(int(bool(causal)), *_int32(window=window),
                                 self._dense(sinks, "sinks", torch.float32, (self.heads,)) if sinks is not None else None)
         lp = self._dense(lse, "lse", torch.float32, (T, self.heads)) if lse is not None else None
         self._call("moe_paged_attention", qp, ldq, T, pages, batch, opt, op, ldo, lp)

@@ -55,3 +55,18 @@ def test_contexts_of_the_same_layout_share_pages():
         for f in calls(b, pages, batch):
             with pytest.raises(ValueError, match="the kernels run on a GPU"):
                 f()
+
+
+def test_sizes_past_32_bits_are_refused():
+    """Their lower bits alone would be legal sizes: a window of 2^32 + 5 would be one of 5."""
+    ctx = make()
+    pages, batch = cache(ctx)
+    q = torch.zeros(3, 4, 32)
+    for window in (2 ** 32 + 5, 2 ** 32, 2 ** 31, -2 ** 32 + 1):
+        with pytest.raises(ValueError, match="does not fit 32 bits"):
+            ctx.moe_paged_attention(q, pages, batch, window=window)
+    for name, v in (("heads", 4), ("kv_heads", 2), ("dim", 32), ("page", 8)):
+        with pytest.raises(ValueError, match="does not fit 32 bits"):
+            make(**{name: 2 ** 32 + v})
+    with pytest.raises(ValueError, match="does not fit 32 bits"):
+        binding.kv_workspace_bytes(2 ** 32 + 4, 2, 32, 8, torch.float32)
