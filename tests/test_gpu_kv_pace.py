@@ -8,6 +8,7 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 
 
+# (measured, us, 4096 slots: sequences one by one 414, by halves 4.0, neighbours 2.9)
 @pytest.mark.parametrize("S", [256, 4096, 65536])
 def test_rows_of_slots_far_apart(gpu_lib, S):
     """Four rows of a wave in the first and the last of many slots, the ones between empty, beside four in the first two."""
