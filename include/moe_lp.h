@@ -315,7 +315,9 @@ moe_status moe_set_ffn_variant(moe_ctx *ctx, int32_t variant);
  * is negative, because kv_lens[s] is less than the sequence's rows, the row is not written, and sees nothing under a causal mask.)
  * Descriptors live on the device and are read by every call, so a captured graph replays with what they then hold.  Row offsets that
  * descend or leave [0, T] make moe_paged_attention compute nothing; no descriptor makes a call touch memory outside its tensors.
- * Limits (MOE_ERR_SHAPE): T * heads <= 2^30, max_pages * page <= 2^30, n_seqs < 2^22, n_pages < 2^31.
+ * Limits (MOE_ERR_SHAPE): T * heads <= 2^30, max_pages * page <= 2^30, n_seqs < 2^22, n_pages < 2^31, and less than 2^24 blocks of 256
+ * threads to a launch (attention: a block for a key/value head of a sequence that can have rows, for every 16 to 128 packed rows more, and for
+ * every piece; append and gather: 16 bytes of a row to a lane, and four vectors).
  */
 typedef enum { MOE_KV_DTYPE = 0, MOE_KV_FP8 = 1 } moe_kv_format;
 

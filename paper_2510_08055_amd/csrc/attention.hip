@@ -45,59 +45,61 @@ template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> __global__ __lau
     Few<T, FP8, DP, 1, EXACT>::run(a, it, *reinterpret_cast<typename Few<T, FP8, DP, 1, EXACT>::Shared*>(smem));
 }
 
-template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> hipError_t launch(AttnArgs a, hipStream_t s)
+template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> hipError_t launch(AttnArgs a, bool clear_tickets, hipStream_t s)
 {
     typedef Kernel<T, FP8, DP, EXACT, LIGHT> K;
     a.few_rows = K::NQ * 16;
     a.tile_rows = K::MANY ? kManyRows : a.few_rows;
     a.tile_tokens = a.tile_rows / a.G;
+    // a block for every item there can be: a tile for a sequence and for tile_rows more packed rows
+    const int64_t tiles = (int64_t)(a.c.S < a.c.T ? a.c.S : a.c.T) + (int64_t)a.c.T * a.G / a.tile_rows;
+    const int64_t base = tiles * a.c.Hk;
+    if (base > kMaxBlocks) return hipErrorInvalidConfiguration;
     int units = 0;
     hipError_t e = compute_units(&units);
     if (e != hipSuccess) return e;
     a.tile_items = units * K::BLOCKS;
     a.g_magic = map_magic_of(a.G);
     a.hk_magic = map_magic_of(a.c.Hk);
-    // a block for every item there can be: a tile for a sequence and for tile_rows more packed rows; pieces are kFewItems and tile_items
-    // more at most (and a few for the rounding of their lengths), fewer where no history is long
-    const int64_t tiles = (int64_t)(a.c.S < a.c.T ? a.c.S : a.c.T) + (int64_t)a.c.T * a.G / a.tile_rows;
-    const int64_t base = tiles * a.c.Hk;
+    // pieces are kFewItems and tile_items more at most (and a few for the rounding of their lengths), fewer where no history is long
     const int64_t longest = (int64_t)a.c.max_pages << a.c.page_shift;
     const int64_t by_length = longest > kMinPiece ? base * ((longest - 1) / kMinPiece) : 0;
     const int64_t most = kFewItems + a.tile_items + 64;
     const int64_t grid = base + (by_length < most ? by_length : most) + 16;      // (those of many rows are rounded up to eights)
-    if (grid > 0x7fffffff) return hipErrorInvalidValue;
+    if (grid > kMaxBlocks) return hipErrorInvalidConfiguration;
     static bool done[kMaxDevices];
     const auto kern = attention_kernel<T, FP8, DP, EXACT, LIGHT>;
     e = ensure_lds_limit(kern, K::LDS, done);
     if (e != hipSuccess) return e;
+    if (clear_tickets && (e = launch_fill_zero(a.tickets, kPartUnits, s)) != hipSuccess) return e;
     kern<<<(unsigned)grid, 256, K::LDS, s>>>(a);
     return hipGetLastError();
 }
 
-template <typename T, bool FP8, int DP> hipError_t launch_by_rows(const AttnArgs& a, hipStream_t s)
+template <typename T, bool FP8, int DP> hipError_t launch_by_rows(const AttnArgs& a, bool clear, hipStream_t s)
 {
     // How rows spread over the sequences only the device knows; with no more than 16 packed rows to a sequence on average, a batch is
     // taken for one of decode rows.  (Right for any spread: a sequence with more rows has more tiles.)
     const bool light = (int64_t)a.c.T * a.G <= (int64_t)16 * a.c.S;
     if constexpr (sizeof(T) == 2) {
-        if (a.c.D == DP) return light ? launch<T, FP8, DP, true, true>(a, s) : launch<T, FP8, DP, true, false>(a, s);
+        if (a.c.D == DP) return light ? launch<T, FP8, DP, true, true>(a, clear, s) : launch<T, FP8, DP, true, false>(a, clear, s);
     }
-    return light ? launch<T, FP8, DP, false, true>(a, s) : launch<T, FP8, DP, false, false>(a, s);
+    return light ? launch<T, FP8, DP, false, true>(a, clear, s) : launch<T, FP8, DP, false, false>(a, clear, s);
 }
 
-template <typename T, bool FP8> hipError_t launch_by_dim(const AttnArgs& a, hipStream_t s)
+template <typename T, bool FP8> hipError_t launch_by_dim(const AttnArgs& a, bool clear, hipStream_t s)
 {
-    if (a.c.D <= 64) return launch_by_rows<T, FP8, 64>(a, s);
-    if (a.c.D <= 128) return launch_by_rows<T, FP8, 128>(a, s);
-    return launch_by_rows<T, FP8, 256>(a, s);
+    if (a.c.D <= 64) return launch_by_rows<T, FP8, 64>(a, clear, s);
+    if (a.c.D <= 128) return launch_by_rows<T, FP8, 128>(a, clear, s);
+    return launch_by_rows<T, FP8, 256>(a, clear, s);
 }
 
 }  // namespace
 
-hipError_t launch_attention(int dtype, bool fp8, const AttnArgs& a, hipStream_t s)
+hipError_t launch_attention(int dtype, bool fp8, const AttnArgs& a, bool clear, hipStream_t s)
 {
-    if (dtype == MOE_BF16) return fp8 ? launch_by_dim<bf16_t, true>(a, s) : launch_by_dim<bf16_t, false>(a, s);
-    return fp8 ? launch_by_dim<float, true>(a, s) : launch_by_dim<float, false>(a, s);
+    if (dtype == MOE_BF16) return fp8 ? launch_by_dim<bf16_t, true>(a, clear, s) : launch_by_dim<bf16_t, false>(a, clear, s);
+    return fp8 ? launch_by_dim<float, true>(a, clear, s) : launch_by_dim<float, false>(a, clear, s);
 }
 
 }  // namespace moe

@@ -27,6 +27,9 @@ __device__ __forceinline__ float scale_of(uint32_t byte)
     return byte == 255u ? __builtin_nanf("") : f;
 }
 
+// A launch has fewer than 2^32 threads, in blocks of 256 here.  What takes more is not launched: hipErrorInvalidConfiguration.
+constexpr int64_t kMaxBlocks = ((int64_t)1 << 24) - 1;
+
 // kv_cache.hip
 hipError_t launch_kv_append(int dtype, bool fp8, const KVView& c, const void* k, int64_t ldk, const void* v, int64_t ldv, hipStream_t s);
 hipError_t launch_kv_gather(int dtype, bool fp8, const KVView& c, void* k, int64_t ldk, void* v, int64_t ldv, hipStream_t s);
@@ -51,6 +54,7 @@ struct AttnArgs {
 };
 // Partial results are stored in units of 16 rows.
 constexpr int kPartUnits = 8192;
-hipError_t launch_attention(int dtype, bool fp8, const AttnArgs& a, hipStream_t s);
+// clear_tickets: they are not known to be zero
+hipError_t launch_attention(int dtype, bool fp8, const AttnArgs& a, bool clear_tickets, hipStream_t s);
 
 }  // namespace moe

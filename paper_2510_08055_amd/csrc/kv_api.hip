@@ -36,7 +36,7 @@ inline size_t stats_bytes() { return (size_t)kPartUnits * 16 * sizeof(float2); }
 inline size_t workspace_size(const moe_kv_config& c) { return part_bytes(c) + stats_bytes() + kPartUnits * sizeof(uint32_t); }
 
 inline bool misaligned(const void* p, uintptr_t to = 16) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
-inline moe_status dev(hipError_t e) { return e == hipSuccess ? MOE_OK : MOE_ERR_DEVICE; }
+inline moe_status dev(hipError_t e) { return e == hipSuccess ? MOE_OK : e == hipErrorInvalidConfiguration ? MOE_ERR_SHAPE : MOE_ERR_DEVICE; }
 
 // Rows of a tensor: `width` elements, ld apart, 16-byte aligned.
 moe_status check_rows(const moe_kv_config& g, const void* p, int64_t ld, int64_t width)
@@ -173,18 +173,17 @@ moe_status moe_paged_attention(moe_kv_ctx* ctx, const void* q, int64_t ldq, int6
     a.part_stats = ctx->part_stats;
     a.tickets = ctx->tickets;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (!ctx->tickets_clear) {
-        // The tickets are zero between launches once they have been cleared: in front of a context's first call.  A call that is
-        // being captured carries the clear along, runs when its graph is replayed, and so leaves it to the next call as well.
-        hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-        if (hipStreamIsCapturing(s, &capture) != hipSuccess) {
-            (void)hipGetLastError();        // (the legacy stream while another one is captured)
-            capture = hipStreamCaptureStatusActive;
-        }
-        if (launch_fill_zero(ctx->tickets, kPartUnits, s) != hipSuccess) return MOE_ERR_DEVICE;
-        ctx->tickets_clear = capture == hipStreamCaptureStatusNone;
+    // The tickets are zero between launches once they have been cleared: in front of a context's first call.  A call that is
+    // being captured carries the clear along, runs when its graph is replayed, and so leaves it to the next call as well.
+    const bool clear = !ctx->tickets_clear;
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (clear && hipStreamIsCapturing(s, &capture) != hipSuccess) {
+        (void)hipGetLastError();        // (the legacy stream while another one is captured)
+        capture = hipStreamCaptureStatusActive;
     }
-    return dev(launch_attention(g.dtype, g.kv_format == MOE_KV_FP8, a, s));
+    st = dev(launch_attention(g.dtype, g.kv_format == MOE_KV_FP8, a, clear, s));
+    if (clear) ctx->tickets_clear = st == MOE_OK && capture == hipStreamCaptureStatusNone;
+    return st;
 }
 
 }  // extern "C"

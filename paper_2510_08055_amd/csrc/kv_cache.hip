@@ -250,18 +250,18 @@ template <typename T, int LPR> __global__ __launch_bounds__(256) void gather_fp8
     }
 }
 
-// Lanes to a vector of n pieces: the next power of two, 8 at least.
-template <typename F> hipError_t by_lanes(int n, F f)
+// f with the lanes to a vector of n pieces (the next power of two, 8 at least) and the blocks that they take for the batch.
+template <typename F> hipError_t by_lanes(const KVView& c, int n, F f)
 {
-    if (n <= 8) return f(std::integral_constant<int, 8>());
-    if (n <= 16) return f(std::integral_constant<int, 16>());
-    if (n <= 32) return f(std::integral_constant<int, 32>());
-    return f(std::integral_constant<int, 64>());
-}
-inline unsigned blocks_for(const KVView& c, int lanes)
-{
-    const int64_t groups = ((int64_t)c.T * lanes + 63) / 64, parts = (2 * c.Hk + R - 1) / R;
-    return (unsigned)((groups * parts + 3) / 4);
+    auto with = [&](auto lanes) {
+        const int64_t groups = ((int64_t)c.T * decltype(lanes)::value + 63) / 64, parts = (2 * c.Hk + R - 1) / R;
+        const int64_t blocks = (groups * parts + 3) / 4;
+        return blocks <= kMaxBlocks ? f(lanes, (unsigned)blocks) : hipErrorInvalidConfiguration;
+    };
+    if (n <= 8) return with(std::integral_constant<int, 8>());
+    if (n <= 16) return with(std::integral_constant<int, 16>());
+    if (n <= 32) return with(std::integral_constant<int, 32>());
+    return with(std::integral_constant<int, 64>());
 }
 
 }  // namespace
@@ -270,17 +270,17 @@ hipError_t launch_kv_append(int dtype, bool fp8, const KVView& c, const void* k,
 {
     const int esz = dtype == MOE_BF16 ? 2 : 4;
     if (!fp8)
-        return by_lanes(c.D * esz / 16, [&](auto lpr) {
+        return by_lanes(c, c.D * esz / 16, [&](auto lpr, unsigned blocks) {
             constexpr int L = decltype(lpr)::value;
-            append_kernel<L><<<blocks_for(c, L), 256, 0, s>>>(c, static_cast<const char*>(k), ldk, static_cast<const char*>(v), ldv, esz);
+            append_kernel<L><<<blocks, 256, 0, s>>>(c, static_cast<const char*>(k), ldk, static_cast<const char*>(v), ldv, esz);
             return hipGetLastError();
         });
-    return by_lanes(c.D / 8, [&](auto lpr) {
+    return by_lanes(c, c.D / 8, [&](auto lpr, unsigned blocks) {
         constexpr int L = decltype(lpr)::value;
         if (dtype == MOE_BF16)
-            append_fp8_kernel<bf16_t, L><<<blocks_for(c, L), 256, 0, s>>>(c, static_cast<const bf16_t*>(k), ldk, static_cast<const bf16_t*>(v), ldv);
+            append_fp8_kernel<bf16_t, L><<<blocks, 256, 0, s>>>(c, static_cast<const bf16_t*>(k), ldk, static_cast<const bf16_t*>(v), ldv);
         else
-            append_fp8_kernel<float, L><<<blocks_for(c, L), 256, 0, s>>>(c, static_cast<const float*>(k), ldk, static_cast<const float*>(v), ldv);
+            append_fp8_kernel<float, L><<<blocks, 256, 0, s>>>(c, static_cast<const float*>(k), ldk, static_cast<const float*>(v), ldv);
         return hipGetLastError();
     });
 }
@@ -289,17 +289,17 @@ hipError_t launch_kv_gather(int dtype, bool fp8, const KVView& c, void* k, int64
 {
     const int esz = dtype == MOE_BF16 ? 2 : 4;
     if (!fp8)
-        return by_lanes(c.D * esz / 16, [&](auto lpr) {
+        return by_lanes(c, c.D * esz / 16, [&](auto lpr, unsigned blocks) {
             constexpr int L = decltype(lpr)::value;
-            gather_kernel<L><<<blocks_for(c, L), 256, 0, s>>>(c, static_cast<char*>(k), ldk, static_cast<char*>(v), ldv, esz);
+            gather_kernel<L><<<blocks, 256, 0, s>>>(c, static_cast<char*>(k), ldk, static_cast<char*>(v), ldv, esz);
             return hipGetLastError();
         });
-    return by_lanes(c.D / 8, [&](auto lpr) {
+    return by_lanes(c, c.D / 8, [&](auto lpr, unsigned blocks) {
         constexpr int L = decltype(lpr)::value;
         if (dtype == MOE_BF16)
-            gather_fp8_kernel<bf16_t, L><<<blocks_for(c, L), 256, 0, s>>>(c, static_cast<bf16_t*>(k), ldk, static_cast<bf16_t*>(v), ldv);
+            gather_fp8_kernel<bf16_t, L><<<blocks, 256, 0, s>>>(c, static_cast<bf16_t*>(k), ldk, static_cast<bf16_t*>(v), ldv);
         else
-            gather_fp8_kernel<float, L><<<blocks_for(c, L), 256, 0, s>>>(c, static_cast<float*>(k), ldk, static_cast<float*>(v), ldv);
+            gather_fp8_kernel<float, L><<<blocks, 256, 0, s>>>(c, static_cast<float*>(k), ldk, static_cast<float*>(v), ldv);
         return hipGetLastError();
     });
 }

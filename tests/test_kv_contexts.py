@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2510_08055_amd import binding
+from test_kv_abi import SHAPE, Call
 
 
 def cache(ctx, n=3):
@@ -70,3 +71,15 @@ def test_sizes_past_32_bits_are_refused():
             make(**{name: 2 ** 32 + v})
     with pytest.raises(ValueError, match="does not fit 32 bits"):
         binding.kv_workspace_bytes(2 ** 32 + 4, 2, 32, 8, torch.float32)
+
+
+def test_calls_of_more_blocks_than_a_launch_has_are_refused():
+    """Legal in every other number: 2^30 rows of one head, and 2^22 - 1 sequences of a row of 256 heads."""
+    c = Call(heads=1, kv_heads=1, dim=16)
+    batch = {"n_seqs": 2 ** 22 - 1}
+    assert c.status("append", T=2 ** 30) == SHAPE and c.status("gather", T=2 ** 30) == SHAPE
+    assert c.status("append", T=2 ** 30, batch=batch) == SHAPE
+    for fmt, dtype in ((0, 1), (1, 1), (0, 0), (1, 0)):
+        c = Call(heads=256, kv_heads=256, dim=32, fmt=fmt, dtype=dtype)
+        for what in ("append", "gather", "attention"):
+            assert c.status(what, T=2 ** 22, batch=batch) == SHAPE, (what, fmt, dtype)
