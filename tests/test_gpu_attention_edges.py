@@ -105,3 +105,36 @@ def test_keys_of_minus_infinity_are_weights_of_zero(gpu_lib, dim, rows, group, d
         b.k_pages[int(b.table[0, at // 16]), 0, at % 16, 3] = -math.inf
     out, lse = check(gpu_lib, b)
     assert torch.isfinite(out.float()).all() and torch.isfinite(lse).all()
+
+
+# ---- more pieces than the partial results' workspace holds ----
+
+def units_needed(rows, kv, group, kv_heads, dim, units):
+    """What find_item (attention_plan.h) counts for a bf16 batch of the kernel with tiles of 128 rows: units of 16 rows of partial results."""
+    tiles = [(-(-n * group // 128), 8, True) if n * group > 32 else (1, 1 if n * group <= 16 else 2, False) for n in rows]
+    work = {m: sum(t * k for (t, _, many), k in zip(tiles, kv) if many == m) * kv_heads for m in (False, True)}
+
+    def even(v, items, least):
+        v = v / items
+        return least if v <= least else (int(v) + 128) // 128 * 128
+
+    piece = {False: even(work[False], 512, 128), True: even(work[False] + work[True], 2 * units, 512)}
+    need = 0
+    for (t, u, many), k in zip(tiles, kv):
+        n = -(-k // piece[many])
+        need += t * kv_heads * n * u if n > 1 else 0
+    return need
+
+
+@pytest.mark.parametrize("kv_heads", [8, 4, 1])
+def test_more_pieces_than_the_workspace_holds(gpu_lib, kv_heads):
+    """All of them are off then.  8 / kv_heads times as many sequences: up to 64, up to 256 and more are planned in ways of their own."""
+    many, few = 62 * 8 // kv_heads, 8 // kv_heads
+    rows, kv = [33] * many + [1] * few, [10000] * many + [16000] * few
+    units = torch.cuda.get_device_properties(0).multi_processor_count
+    assert units_needed(rows, kv, 1, kv_heads, 64, units) > 8192, units      # (sizes for 256 compute units)
+    b = Batch(rows, [33] * many + [16000] + [1] * (few - 1), kv_heads, kv_heads, 64, 16, seed=kv_heads)
+    b.table[:] = b.table[many].clone()        # the sequences share their pages
+    b.kv = kv
+    b.kv_lens = torch.tensor(kv, dtype=torch.int32, device=DEV)
+    check(gpu_lib, b)
