@@ -78,9 +78,15 @@ template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> hipError_t launc
 
 template <typename T, bool FP8, int DP> hipError_t launch_by_rows(const AttnArgs& a, bool clear, hipStream_t s)
 {
-    // How rows spread over the sequences only the device knows; with no more than 16 packed rows to a sequence on average, a batch is
-    // taken for one of decode rows.  (Right for any spread: a sequence with more rows has more tiles.)
-    const bool light = (int64_t)a.c.T * a.G <= (int64_t)16 * a.c.S;
+    // How rows spread over the sequences only the device knows.  Either kernel is right for any spread; a batch is taken for one of decode rows
+    // (or drafted ones) with no more than 16 packed rows to a sequence on average, and where no sequence can have more than a few tiles' worth
+    // of them: all but one row of every other sequence, or, with fewer rows than sequences, where empty ones are certain, all rows.
+    // Measured, us, kernel with many-row tiles / the light one.  Batches of decode or drafted rows: dim 128, 64 sequences of up to 7000 tokens, 8 key/value
+    // heads 273 / 259, FP8 164 / 149, 4 of them 155 / 145, FP8 91 / 78; 16 of four drafted rows over up to 1500 tokens 23 / 20, FP8 19 / 15.  Beside
+    // 256 decode rows, 32 heads over 8, a prompt over 7680 tokens of 16 rows 147 / 177, 64 rows 151 / 236, 128 rows 156 / 245, 200 rows 163 / 353, 512 rows 197 / 455.
+    constexpr int kMostRows = 3 * kManyRows;
+    const int64_t rows = a.c.T, seqs = a.c.S, most = rows < seqs ? rows : rows - seqs + 1;
+    const bool light = rows * a.G <= 16 * seqs && most * a.G <= kMostRows;
     if constexpr (sizeof(T) == 2) {
         if (a.c.D == DP) return light ? launch<T, FP8, DP, true, true>(a, clear, s) : launch<T, FP8, DP, true, false>(a, clear, s);
     }
