@@ -360,16 +360,16 @@ class Context:
         _check(self.lib.moe_set_ffn_variant(self._ctx, v), "moe_set_ffn_variant")
 
 
-def _int32(**sizes):
-    """The sizes in their order; ctypes would drop their upper bits without a word."""
-    for name, v in sizes.items():
-        if not -2 ** 31 <= v < 2 ** 31:
-            raise ValueError(f"{name}: {v} does not fit 32 bits")
-    return [int(v) for v in sizes.values()]
+def _int32(name, v):
+    """ctypes would drop its upper bits without a word."""
+    if not -0x80000000 <= v <= 0x7fffffff:
+        raise ValueError(f"{name}: {v} does not fit 32 bits")
+    return int(v)
 
 
 def _kv_config(heads, kv_heads, dim, page, dtype, kv_format):
-    return CKVConfig(*_int32(heads=heads, kv_heads=kv_heads, dim=dim, page=page), _dtype_code(dtype), KV_FORMATS[kv_format])
+    return CKVConfig(_int32("heads", heads), _int32("kv_heads", kv_heads), _int32("dim", dim), _int32("page", page), _dtype_code(dtype),
+                     KV_FORMATS[kv_format])
 
 
 def kv_workspace_bytes(heads, kv_heads, dim, page, dtype, kv_format="") -> int:
@@ -391,6 +391,9 @@ class KVBatch(CKVBatch):
     device = None
 
 
+_the_same = {}       # equal values as one object, so that a call compares identities
+
+
 class KVContext:
     """A moe_kv_ctx plus the torch-allocated workspace it lives on: a paged key/value cache's format and its attention.
 
@@ -410,7 +413,9 @@ class KVContext:
         n = ctypes.c_size_t(0)
         _check(self.lib.moe_kv_workspace_bytes(ctypes.byref(self.cfg), ctypes.byref(n)), "moe_kv_workspace_bytes")
         self.workspace = torch.empty(n.value + 256, dtype=torch.uint8, device=self.device)
-        self.layout = (kv_heads, page, dim, self.page_dtype, self.workspace.device)
+        layout = (kv_heads, page, dim, self.page_dtype, self.workspace.device)
+        self.layout = _the_same.setdefault(layout, layout)
+        self.batch_device = _the_same.setdefault(self.workspace.device, self.workspace.device)
         base = (self.workspace.data_ptr() + 255) // 256 * 256
         self._ctx = ctypes.c_void_p()
         _check(self.lib.moe_kv_create(ctypes.byref(self.cfg), ctypes.c_void_p(base), n.value, ctypes.byref(self._ctx)), "moe_kv_create")
@@ -439,10 +444,10 @@ class KVContext:
 
     def _packed(self, pages, batch):
         """The structs hold pointers alone, so what pack_pages and pack_batch checked has to be what this context reads."""
-        if getattr(pages, "layout", None) != self.layout:
+        if getattr(pages, "layout", None) is not self.layout:
             raise ValueError(f"pages packed for {getattr(pages, 'layout', None)} do not belong to a context of {self.layout}")
-        if getattr(batch, "device", None) != self.workspace.device:
-            raise ValueError(f"a batch packed on {getattr(batch, 'device', None)} does not belong to a context on {self.workspace.device}")
+        if getattr(batch, "device", None) is not self.batch_device:
+            raise ValueError(f"a batch packed on {getattr(batch, 'device', None)} does not belong to a context on {self.batch_device}")
 
     def _dense(self, t, name, dtype, shape):
         if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != self.workspace.device:
@@ -483,7 +488,7 @@ class KVContext:
         b = KVBatch(self._dense(row_offsets, "row_offsets", torch.int32, (n + 1,)), self._dense(kv_lens, "kv_lens", torch.int32, (n,)),
                     self._dense(page_table, "page_table", torch.int32, (n, page_table.shape[1])), n, page_table.shape[1])
         b.tensors = (row_offsets, kv_lens, page_table)
-        b.device = self.workspace.device
+        b.device = self.batch_device
         return b
 
     # ---- the calls of the boundary, same names as the C ABI ----
@@ -517,7 +522,7 @@ class KVContext:
             out = torch.empty((T, self.heads, self.dim), dtype=self.dtype, device=self.device)
         qp, ldq = self._rows(q, "q", T, self.heads)
         op, ldo = self._rows(out, "out", T, self.heads)
-        opt = CAttentionOptions(int(bool(causal)), *_int32(window=window),
+        opt = CAttentionOptions(int(bool(causal)), _int32("window", window),
                                 self._dense(sinks, "sinks", torch.float32, (self.heads,)) if sinks is not None else None)
         lp = self._dense(lse, "lse", torch.float32, (T, self.heads)) if lse is not None else None
         self._call("moe_paged_attention", qp, ldq, T, pages, batch, opt, op, ldo, lp)
