@@ -380,7 +380,8 @@ typedef struct {
  * q, out: T rows of heads * dim elements, ldq and ldo apart; lse [T, heads] fp32 or NULL.  A row that sees nothing gives zeros,
  * and the sink (or minus infinity) as its lse.  bf16 contexts multiply on the matrix cores with fp32 sums, the weights w rounded
  * to bf16 against the maximum; maxima, sums and partial outputs are fp32.  What a row does not see has no part in its result,
- * whatever it holds.  The result of a row is the same bits for the same batch; it may differ in rounding with the other
+ * whatever it holds.  (Sums run over the tokens before they are divided, with weights of up to 2^8: values beyond 2^119 over the number of tokens, about,
+ * give infinities or NaN where their mean would still be finite.)  The result of a row is the same bits for the same batch; it may differ in rounding with the other
  * sequences of the batch, because long histories are split among compute units by the batch's total work.
  */
 moe_status moe_paged_attention(moe_kv_ctx *ctx, const void *q, int64_t ldq, int64_t T, const moe_kv_pages *pages,

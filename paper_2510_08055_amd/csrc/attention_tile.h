@@ -18,8 +18,8 @@ namespace {
 //
 // Why 128 rows and four waves: a step's 32 KB of operands are read from LDS by every wave for its 32 rows, 128 bytes a cycle if the matrix
 // pipes never paused, and two such blocks share a unit, each with its own barrier, so that one's exponentials run beside the other's
-// products.  What bounds it at dim 128: the matrix pipes at the clock that they leave (2.0 GHz), busy 46 % of a causal prompt of 8192 tokens and 32
-// heads (580 us with 128 decode rows, 0.95 PFLOP/s), half of all steps' issue being vector instructions.  8192 rows to 8192 tokens, no
+// products.  What bounds it at dim 128: the matrix pipes at the clock that they leave (2.0 GHz), busy 45 % of a causal prompt of 8192 tokens and 32
+// heads (573 us with 128 decode rows, 0.96 PFLOP/s), half of all steps' issue being vector instructions.  8192 rows to 8192 tokens, no
 // mask, 32 heads: dim 128 1043 us (1.05 PFLOP/s), FP8 pages 1139; dim 64 628 (0.88: as many exponentials for half the products), FP8 666; 4096 to 4096,
 // 16 heads, dim 256, one block to a unit: 420 (0.65).
 // ----------------------------------------------------------------------------------------------------------------
