@@ -84,9 +84,11 @@ template <typename T, bool FP8, int DP> hipError_t launch_by_rows(const AttnArgs
     // Measured, us, kernel with many-row tiles / the light one.  Batches of decode or drafted rows: dim 128, 64 sequences of up to 7000 tokens, 8 key/value
     // heads 273 / 259, FP8 164 / 149, 4 of them 155 / 145, FP8 91 / 78; 16 of four drafted rows over up to 1500 tokens 23 / 20, FP8 19 / 15.  Beside
     // 256 decode rows, 32 heads over 8, a prompt over 7680 tokens of 16 rows 147 / 177, 64 rows 151 / 236, 128 rows 156 / 245, 200 rows 163 / 353, 512 rows 197 / 455.
+    // fp32 batches have no tiles of many rows to lose: there the average alone decides (256 decode rows beside 512 prompt rows, us, tiles of 32 / of 16: dim 128,
+    // 32 heads over 8 410 / 331, over 7680 tokens 1116 / 1122; dim 64, 32 over 32 641 / 532, 1005 / 943).
     constexpr int kMostRows = 3 * kManyRows;
     const int64_t rows = a.c.T, seqs = a.c.S, most = rows < seqs ? rows : rows - seqs + 1;
-    const bool light = rows * a.G <= 16 * seqs && most * a.G <= kMostRows;
+    const bool light = rows * a.G <= 16 * seqs && (sizeof(T) == 4 || most * a.G <= kMostRows);
     if constexpr (sizeof(T) == 2) {
         if (a.c.D == DP) return light ? launch<T, FP8, DP, true, true>(a, clear, s) : launch<T, FP8, DP, true, false>(a, clear, s);
     }
