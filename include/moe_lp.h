@@ -317,7 +317,8 @@ moe_status moe_set_ffn_variant(moe_ctx *ctx, int32_t variant);
  * descend or leave [0, T] make moe_paged_attention compute nothing; no descriptor makes a call touch memory outside its tensors.
  * Limits (MOE_ERR_SHAPE): T * heads <= 2^30, max_pages * page <= 2^30, n_seqs < 2^22, n_pages < 2^31, and less than 2^24 blocks of 256
  * threads to a launch (attention: a block for a key/value head of a sequence that can have rows, for every 16 to 128 packed rows more, and for
- * every piece; append and gather: 16 bytes of a row to a lane, and four vectors).
+ * every piece; append and gather: 16 bytes of a row to a lane, and four vectors; select: four for every sequence and key/value head, compact two).
+ * moe_kv_weights: min(n_seqs, 256) * kv_heads * (max_pages * page / 32 + 1) < 2^31.
  */
 typedef enum { MOE_KV_DTYPE = 0, MOE_KV_FP8 = 1 } moe_kv_format;
 
@@ -387,6 +388,88 @@ typedef struct {
 moe_status moe_paged_attention(moe_kv_ctx *ctx, const void *q, int64_t ldq, int64_t T, const moe_kv_pages *pages,
                                const moe_kv_batch *batch, const moe_attention_options *opt, void *out, int64_t ldo, float *lse,
                                void *stream);
+
+/*
+ * Trees of drafted tokens (several continuations verified in one pass).  A sequence's new rows are then a tree: row i's parent is row
+ * parents[i] < i of the same sequence, or none (-1: a child of what is cached; anything else counts as -1).  Their keys and values are appended as
+ * any rows' are, row i in slot kv_lens - n + i.  Only sequences of up to 64 * words rows are trees; in the same batch longer ones, prompts, are causal
+ * (words: 1..16), and their parents are not read.
+ *
+ * moe_tree_masks turns parents [T] into what the attention reads: masks [T, words], bit j of row i set if j is i or one of its ancestors (bit j of
+ * a row: bit j % 64 of word j / 64), and positions [T], the number of tokens before a row on its path: kv_lens - n + the number of its ancestors (what a
+ * rotary embedding of its query and key needs).  window > 0: ancestors window or more tokens up are left out.  Rows of prompts get
+ * masks of zeros and kv_lens - n + i.  positions may be NULL.  Only row_offsets and kv_lens of the batch are read; rows of no sequence are left as they
+ * were, and so are those of a sequence whose offsets descend or leave [0, T].
+ */
+moe_status moe_tree_masks(moe_kv_ctx *ctx, const int32_t *parents, int64_t T, const moe_kv_batch *batch, int32_t words, int32_t window,
+                          uint64_t *masks, int32_t *positions, void *stream);
+
+typedef struct {
+    const uint64_t *masks;    /* [T, words], 8-byte aligned */
+    const int32_t *positions; /* [T]; may be NULL without a window */
+    int32_t words;            /* 1..16 */
+} moe_tree;
+
+/*
+ * moe_paged_attention of a batch with trees: row i of a tree sees all tokens before the tree's first row, and of the tree's rows those whose bits
+ * its mask has (itself only by its own bit; bits past the sequence's rows count for nothing; a row may see nothing at all).  opt->window: of the tokens
+ * before the tree a row sees those from positions[row] - window + 1 on, positions taken within [kv_lens - n, kv_lens - 1]; among the tree's rows the mask alone
+ * decides.  opt->causal must be 1: it is what longer sequences are.  Everything else is as for moe_paged_attention.
+ */
+moe_status moe_tree_attention(moe_kv_ctx *ctx, const void *q, int64_t ldq, int64_t T, const moe_kv_pages *pages, const moe_kv_batch *batch,
+                              const moe_tree *tree, const moe_attention_options *opt, void *out, int64_t ldo, float *lse, void *stream);
+
+typedef struct {
+    int32_t causal, window; /* as in moe_attention_options */
+    float decay;            /* 0..1: what is left of the earlier score of a token */
+} moe_weights_options;
+
+/*
+ * The attention weight that every token and key/value head receives from the new rows, added to its score: scores [n_pages, kv_heads, page] fp32, laid
+ * out as the scale bytes are.
+ *   w_j = sum over the rows that see token j, and over the query heads of its key/value head, of exp(q . k_j / sqrt(dim) - lse),
+ *   score_j = w_j for the tokens of the new rows themselves, decay * score_j + w_j for those before them
+ * for every token j that is there, of the sequences that bring rows; with decay 0 no earlier score is read (it may be anything).  lse [T, heads] fp32 is what moe_paged_attention (with the same
+ * causal and window) left: the w_j of a row are then its softmax weights, less the sink's share.  A row whose lse is minus infinity saw nothing and
+ * adds nothing.  Only the keys of the pages are read.  Scores, exponentials and sums are fp32, in an order that depends on the batch alone: the same call
+ * gives the same bits.  Rows may be the last ones of a prompt whose other rows are cached already, so that those alone are its judges.
+ */
+moe_status moe_kv_weights(moe_kv_ctx *ctx, const void *q, int64_t ldq, const float *lse, int64_t T, const moe_kv_pages *pages,
+                          const moe_kv_batch *batch, const moe_weights_options *opt, float *scores, void *stream);
+
+typedef struct {
+    int32_t budget; /* tokens that a sequence may keep, 1 or more */
+    int32_t first;  /* of these, the first tokens of the sequence */
+    int32_t recent; /* and its last ones; first + recent <= budget */
+} moe_select_options;
+
+/*
+ * Which tokens of every sequence and key/value head to keep: of those that are there, `budget`, or all if there are no more.  Kept are tokens before
+ * `first` and from kv_lens - recent on, then those of the highest scores, equal scores by the lower token; a NaN counts as minus infinity.
+ * keep [n_seqs, kv_heads, budget] int32: the kept tokens, ascending, and -1 behind them; keep_lens [n_seqs] int32: how many (the same for all heads).
+ * scores [n_pages, kv_heads, page] as above.  Of the batch kv_lens and page_table are read (row_offsets may be NULL).
+ */
+moe_status moe_kv_select(moe_kv_ctx *ctx, const float *scores, int64_t n_pages, const moe_kv_batch *batch, const moe_select_options *opt,
+                         int32_t *keep, int32_t *keep_lens, void *stream);
+
+typedef struct {
+    const int32_t *tokens; /* [n_seqs, kv_heads, max_keep], or [n_seqs, max_keep] for all heads alike */
+    const int32_t *lens;   /* [n_seqs]: how many of them count (no more than max_keep do) */
+    const int32_t *first;  /* [n_seqs]: the slot that the first one moves to; NULL: 0 */
+    int64_t max_keep;
+    int32_t per_head;      /* 1 or 0: which of the two */
+} moe_kv_keep;
+
+/*
+ * Moves what is kept together, in place: token first[s] + i of a sequence and head becomes what its token tokens[.., i] was, for i = 0 .. lens[s] - 1: keys,
+ * values, scale bytes and, unless scores is NULL, scores.  The sequence then holds first[s] + lens[s] tokens (the caller's to store as kv_lens); what is behind
+ * them is left as it was.  After moe_kv_select keep_lens are the new lengths; after a verified tree `first` is kv_lens - n, and tokens are that plus the
+ * accepted rows.  Tokens must ascend, no token below first[s] + i at place i, as a list of kept ones always does; where one does not, or is
+ * not there, what its place then holds is unspecified (nothing outside the sequence's own pages is touched, whatever the lists hold).  Positions are not
+ * part of a cache: a window counts the tokens that are left.  Pages that several sequences share must not be moved in.
+ */
+moe_status moe_kv_compact(moe_kv_ctx *ctx, const moe_kv_pages *pages, const moe_kv_batch *batch, const moe_kv_keep *keep, float *scores,
+                          void *stream);
 
 const char *moe_status_string(moe_status s);
 

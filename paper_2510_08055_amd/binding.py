@@ -27,7 +27,7 @@ EXPORTS = ["moe_workspace_bytes", "moe_create", "moe_destroy", "moe_router_topk"
            "moe_stack_forward", "moe_read_counters", "moe_reset_counters",
            "moe_kernel_timing", "moe_read_kernel_timing", "moe_ffn_variant", "moe_set_ffn_variant",
            "moe_status_string", "moe_kv_workspace_bytes", "moe_kv_create", "moe_kv_destroy", "moe_kv_append", "moe_kv_gather",
-           "moe_paged_attention"]
+           "moe_paged_attention", "moe_tree_masks", "moe_tree_attention", "moe_kv_weights", "moe_kv_select", "moe_kv_compact"]
 
 FFN_VARIANTS = {"auto": 0, "tile128": 1, "small": 2, "big": 3, "w4_tile64": 4, "w4_stream": 5, "w4_big": 6, "few": 7, "wide": 8}
 
@@ -86,6 +86,23 @@ class CAttentionOptions(ctypes.Structure):
     _fields_ = [("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_void_p)]
 
 
+class CTree(ctypes.Structure):
+    _fields_ = [("masks", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("words", ctypes.c_int32)]
+
+
+class CWeightsOptions(ctypes.Structure):
+    _fields_ = [("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("decay", ctypes.c_float)]
+
+
+class CSelectOptions(ctypes.Structure):
+    _fields_ = [("budget", ctypes.c_int32), ("first", ctypes.c_int32), ("recent", ctypes.c_int32)]
+
+
+class CKVKeep(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("first", ctypes.c_void_p), ("max_keep", ctypes.c_int64),
+                ("per_head", ctypes.c_int32)]
+
+
 @dataclass
 class Counters:
     expert_bytes: int
@@ -133,6 +150,11 @@ def load():
     L.moe_kv_append.argtypes = [vp, vp, i64, vp, i64, i64, pages, batch, vp]
     L.moe_kv_gather.argtypes = [vp, pages, batch, i64, vp, i64, vp, i64, vp]
     L.moe_paged_attention.argtypes = [vp, vp, i64, i64, pages, batch, ctypes.POINTER(CAttentionOptions), vp, i64, vp, vp]
+    L.moe_tree_masks.argtypes = [vp, vp, i64, batch, i32, i32, vp, vp, vp]
+    L.moe_tree_attention.argtypes = [vp, vp, i64, i64, pages, batch, ctypes.POINTER(CTree), ctypes.POINTER(CAttentionOptions), vp, i64, vp, vp]
+    L.moe_kv_weights.argtypes = [vp, vp, i64, vp, i64, pages, batch, ctypes.POINTER(CWeightsOptions), vp, vp]
+    L.moe_kv_select.argtypes = [vp, vp, i64, batch, ctypes.POINTER(CSelectOptions), vp, vp, vp]
+    L.moe_kv_compact.argtypes = [vp, pages, batch, ctypes.POINTER(CKVKeep), vp, vp]
     L.moe_status_string.argtypes = [i32]
     L.moe_status_string.restype = ctypes.c_char_p
     for name in EXPORTS:
@@ -446,6 +468,9 @@ class KVContext:
         """The structs hold pointers alone, so what pack_pages and pack_batch checked has to be what this context reads."""
         if getattr(pages, "layout", None) is not self.layout:
             raise ValueError(f"pages packed for {getattr(pages, 'layout', None)} do not belong to a context of {self.layout}")
+        self._packed_batch(batch)
+
+    def _packed_batch(self, batch):
         if getattr(batch, "device", None) is not self.batch_device:
             raise ValueError(f"a batch packed on {getattr(batch, 'device', None)} does not belong to a context on {self.batch_device}")
 
@@ -527,3 +552,70 @@ class KVContext:
         lp = self._dense(lse, "lse", torch.float32, (T, self.heads)) if lse is not None else None
         self._call("moe_paged_attention", qp, ldq, T, pages, batch, opt, op, ldo, lp)
         return out
+
+    def moe_tree_masks(self, parents, batch, words=1, window=0, masks=None, positions=None):
+        """Ancestor masks [T, words] (int64, 64 bits a word) and positions [T] int32 of trees of drafted tokens.  parents [T] int32: of a row,
+        the row of its sequence that it follows, or -1.  Sequences of more than 64 * words rows are prompts."""
+        self._packed_batch(batch)
+        T = parents.shape[0]
+        if masks is None:
+            masks = torch.empty((T, words), dtype=torch.int64, device=self.device)
+        if positions is None:
+            positions = torch.empty((T,), dtype=torch.int32, device=self.device)
+        self._call("moe_tree_masks", self._dense(parents, "parents", torch.int32, (T,)), T, batch, _int32("words", words), _int32("window", window),
+                   self._dense(masks, "masks", torch.int64, (T, words)), self._dense(positions, "positions", torch.int32, (T,)))
+        return masks, positions
+
+    def moe_tree_attention(self, q, pages, batch, masks, positions=None, window=0, sinks=None, out=None, lse=None):
+        """moe_paged_attention of a batch whose sequences of up to 64 * masks.shape[1] rows are trees (moe_tree_masks); longer ones are
+        causal.  positions are needed with a window."""
+        self._packed(pages, batch)
+        T = q.shape[0]
+        if out is None:
+            out = torch.empty((T, self.heads, self.dim), dtype=self.dtype, device=self.device)
+        qp, ldq = self._rows(q, "q", T, self.heads)
+        op, ldo = self._rows(out, "out", T, self.heads)
+        words = masks.shape[1] if masks.dim() == 2 else 0
+        tree = CTree(self._dense(masks, "masks", torch.int64, (T, words)),
+                     self._dense(positions, "positions", torch.int32, (T,)) if positions is not None else None, words)
+        opt = CAttentionOptions(1, _int32("window", window),
+                                self._dense(sinks, "sinks", torch.float32, (self.heads,)) if sinks is not None else None)
+        lp = self._dense(lse, "lse", torch.float32, (T, self.heads)) if lse is not None else None
+        self._call("moe_tree_attention", qp, ldq, T, pages, batch, tree, opt, op, ldo, lp)
+        return out
+
+    def moe_kv_weights(self, q, lse, pages, batch, scores, causal=True, window=0, decay=1.0):
+        """Adds the attention weights of the rows to scores [n_pages, kv_heads, page] fp32, in place; lse as moe_paged_attention left it."""
+        self._packed(pages, batch)
+        T = q.shape[0]
+        qp, ldq = self._rows(q, "q", T, self.heads)
+        lp = self._dense(lse, "lse", torch.float32, (T, self.heads))
+        sp = self._dense(scores, "scores", torch.float32, (pages.n_pages, self.kv_heads, self.page))
+        self._call("moe_kv_weights", qp, ldq, lp, T, pages, batch, CWeightsOptions(int(bool(causal)), _int32("window", window), decay), sp)
+        return scores
+
+    def moe_kv_select(self, scores, batch, budget, first=0, recent=0, keep=None, keep_lens=None):
+        """The tokens to keep [n_seqs, kv_heads, budget] int32, ascending, -1 behind them, and how many [n_seqs]."""
+        self._packed_batch(batch)
+        shape = (batch.n_seqs, self.kv_heads, _int32("budget", budget))
+        if keep is None:
+            keep = torch.empty(shape, dtype=torch.int32, device=self.device)
+        if keep_lens is None:
+            keep_lens = torch.empty(shape[:1], dtype=torch.int32, device=self.device)
+        n = scores.shape[0]
+        opt = CSelectOptions(shape[2], _int32("first", first), _int32("recent", recent))
+        self._call("moe_kv_select", self._dense(scores, "scores", torch.float32, (n, self.kv_heads, self.page)), n, batch, opt,
+                   self._dense(keep, "keep", torch.int32, shape), self._dense(keep_lens, "keep_lens", torch.int32, shape[:1]))
+        return keep, keep_lens
+
+    def moe_kv_compact(self, pages, batch, keep, keep_lens, first=None, scores=None):
+        """Moves the kept tokens together, from slot first[s] on (0 without): keep [n_seqs, kv_heads, max_keep] int32, or [n_seqs, max_keep] for
+        all heads alike.  The sequences then hold first + keep_lens tokens."""
+        self._packed(pages, batch)
+        n = batch.n_seqs
+        per_head = keep.dim() == 3
+        shape = (n, self.kv_heads, keep.shape[2]) if per_head else (n, keep.shape[-1])
+        lists = CKVKeep(self._dense(keep, "keep", torch.int32, shape), self._dense(keep_lens, "keep_lens", torch.int32, (n,)),
+                        self._dense(first, "first", torch.int32, (n,)) if first is not None else None, shape[-1], int(per_head))
+        sp = self._dense(scores, "scores", torch.float32, (pages.n_pages, self.kv_heads, self.page)) if scores is not None else None
+        self._call("moe_kv_compact", pages, batch, lists, sp)

@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmoe_lp.so")
 SOURCES = ["api.hip", "router.hip", "permute.hip", "ffn.hip", "ffn_w4.hip", "combine.hip", "kv_api.hip", "kv_cache.hip",
-           "attention.hip"]
+           "attention.hip", "tree_attention.hip", "kv_tree.hip", "kv_weights.hip", "kv_select.hip", "kv_compact.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
@@ -44,7 +44,7 @@ def _scratch_users(log, names):
 # load).  The compiler does not honour an M0 clobber on an asm statement, so these files must hold no other
 # use of M0; the build reads the device assembly (a by-product of the same compile) and checks that M0
 # only ever appears as  s_mov_b32 m0, <sgpr> ; s_nop 0 ; global_load_lds_<size>.
-M0_ONLY_FOR_LDS_LOADS = ("ffn.hip", "ffn_w4.hip", "attention.hip")
+M0_ONLY_FOR_LDS_LOADS = ("ffn.hip", "ffn_w4.hip", "attention.hip", "tree_attention.hip")
 
 
 def _foreign_m0_uses(asm):

@@ -38,7 +38,7 @@ __device__ __forceinline__ float sum_over_tokens(float v)
 // a SIMD's share of the memory.
 // ----------------------------------------------------------------------------------------------------------------
 // EXACT: the heads are DP wide, no less, and every offset within a row is a constant.
-template <typename T, bool FP8, int DP, int NQ, bool EXACT> struct Few {
+template <typename T, bool FP8, int DP, int NQ, bool EXACT, bool TREE> struct Few {
     static constexpr bool F32 = sizeof(T) == 4;
     static constexpr int NJ = F32 ? 1 : 2, TOK = NJ * 16;          // 16-token subtiles of a step
     static constexpr int ESZ = FP8 ? 1 : (int)sizeof(T);
@@ -62,7 +62,7 @@ template <typename T, bool FP8, int DP, int NQ, bool EXACT> struct Few {
 
     static __device__ __forceinline__ void run(const AttnArgs& a, const Item& it, Shared& sh)
     {
-        const Range rg = range_of(a, it);
+        const Range rg = range_of<TREE>(a, it);
         if (it.sub >= rg.pieces) return;
         const int lane = lane_id(), n = lane & 15, g = lane >> 4;
         const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -77,14 +77,13 @@ template <typename T, bool FP8, int DP, int NQ, bool EXACT> struct Few {
         if (t0 < t1) pages.hold(a.c, it.seq, t0 >> shift, t1);
 
         // rows: what each sees, and its queries
-        int see_lo[NQ], see_hi[NQ];
+        Sight<TREE> sight[NQ];
         Queries Q;
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
-            const Row r = row_of(a, it, rg, rg.first + i * 16 + n);
+            const auto r = row_of<TREE>(a, it, rg, rg.first + i * 16 + n);
             const bool there = r.there;
-            see_hi[i] = r.see_hi;
-            see_lo[i] = r.see_lo;
+            sight[i] = r.sight;
             const T* src = static_cast<const T*>(a.q) + (int64_t)r.row * a.ldq + (int64_t)r.head * D;
             if constexpr (F32) {
 #pragma unroll
@@ -242,6 +241,10 @@ template <typename T, bool FP8, int DP, int NQ, bool EXACT> struct Few {
             // (a masked step loads the next keys at its end: what it may have to do needs the registers)
             if (more && !masked) load_k(t + TOK);
 
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) sight[i].step(a, t);
+            }
             float p[NQ][NJ][4];
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
@@ -254,7 +257,7 @@ template <typename T, bool FP8, int DP, int NQ, bool EXACT> struct Few {
                         if constexpr (F32 && FP8) x *= kscale[j][r];
                         if (masked) {
                             const int tok = t + j * 16 + g * 4 + r;
-                            if (!(vid[j] >= 0 && tok < see_hi[i] && tok >= see_lo[i])) x = -__builtin_inff();
+                            if (!((vid[j] >= 0) & sight[i].sees(tok))) x = -__builtin_inff();
                         }
                         p[i][j][r] = x;
                         top = fmaxf(top, x);
@@ -292,7 +295,7 @@ template <typename T, bool FP8, int DP, int NQ, bool EXACT> struct Few {
                             if (none) vs[j] = (vs[j] & ~(255u << (8 * r))) | (127u << (8 * r));
                         }
                     }
-                clean_values(a, it, rg, t, see_lo, see_hi, vr, vs, o);
+                clean_values(a, it, rg, t, sight, vr, vs, o);
             }
             if constexpr (FP8) {        // a value's scale goes to its weight: exact, and one product instead of dim
 #pragma unroll
@@ -339,7 +342,7 @@ template <typename T, bool FP8, int DP, int NQ, bool EXACT> struct Few {
             }
             __syncthreads();
             const int q = threadIdx.x >> 4;
-            const Row r = row_of(a, it, rg, rg.first + i * 16 + q);
+            const auto r = row_of<TREE>(a, it, rg, rg.first + i * 16 + q);
             if (r.there) {
                 float M = kLowest, L = 0;
 #pragma unroll
@@ -366,7 +369,7 @@ template <typename T, bool FP8, int DP, int NQ, bool EXACT> struct Few {
                 }
             }
         }
-        if (rg.pieces > 1) join_pieces<T, DP, NQ>(a, it, rg, D, &sh.flag);
+        if (rg.pieces > 1) join_pieces<T, DP, NQ, TREE>(a, it, rg, D, &sh.flag);
     }
 
     // The weights as the second product's operand.  bf16: rounded to nearest, 2^-8 of a weight at most; the sum they are divided by is that
@@ -458,8 +461,8 @@ template <typename T, bool FP8, int DP, int NQ, bool EXACT> struct Few {
             return ((v & 0x7f80u) == 0x7f80u ? 0u : v & 0xffffu) | ((v & 0x7f800000u) == 0x7f800000u ? 0u : v & 0xffff0000u);
         }
     }
-    static __device__ __forceinline__ void clean_values(const AttnArgs& a, const Item& it, const Range& rg, int t, const int (&see_lo)[NQ],
-                                                        const int (&see_hi)[NQ], uint32_t (&vr)[VDW][NJ * 4], uint32_t (&vs)[NJ],
+    static __device__ __forceinline__ void clean_values(const AttnArgs& a, const Item& it, const Range& rg, int t, const Sight<TREE> (&sight)[NQ],
+                                                        uint32_t (&vr)[VDW][NJ * 4], uint32_t (&vs)[NJ],
                                                         float4_t (&o)[VDW][NQ][PER])
     {
         bool any = false;
@@ -505,7 +508,7 @@ template <typename T, bool FP8, int DP, int NQ, bool EXACT> struct Few {
                         const bool odd = (__float_as_uint(f) & 0x7f800000u) == 0x7f800000u;
 #pragma unroll
                         for (int i = 0; i < NQ; ++i)
-                            if (odd && tok < see_hi[i] && tok >= see_lo[i]) o[x][i][y][r] += f;
+                            if (odd & sight[i].sees(tok)) o[x][i][y][r] += f;
                     }
             }
         }

@@ -26,6 +26,7 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 constexpr int kFewItems = 512;
 constexpr int kMinPiece = 128, kMinTilePiece = 512;
 
+// TREE, here and below: the batch's short sequences are drafts whose rows see their ancestors (AttnArgs::masks) instead of all rows before them.
 struct Seq {
     int row0, n, kv;                // first row, rows, tokens with them (of which the table need not reach all: held_of)
     int tiles, units, len;          // tiles of packed rows, units of 16 rows to a tile, tokens of the longest tile's range
@@ -46,7 +47,9 @@ __device__ __forceinline__ int held_of(const KVView& c, int kv)
     return kv < most ? kv : most;
 }
 
-__device__ __forceinline__ Seq shape_of(const AttnArgs& a, int lo, int hi, int kv)
+template <bool TREE> __device__ __forceinline__ bool is_tree(const AttnArgs& a, int n) { return TREE && n <= 64 * a.words; }
+
+template <bool TREE> __device__ __forceinline__ Seq shape_of(const AttnArgs& a, int lo, int hi, int kv)
 {
     Seq q;
     q.row0 = lo;
@@ -62,7 +65,7 @@ __device__ __forceinline__ Seq shape_of(const AttnArgs& a, int lo, int hi, int k
         const int first = q.kv - q.n - a.window + 1;
         int len = q.len - (first > 0 ? first : 0) + 31;
         const int one = a.window + a.tile_tokens + 2 + 31;
-        if (a.causal && one < len) len = one;
+        if (a.causal && !is_tree<TREE>(a, q.n) && one < len) len = one;
         if (len < q.len) q.len = len > 0 ? len : 0;
     }
     return q;
@@ -88,7 +91,7 @@ struct PlanShared {
 // block of a launch runs it before it can load anything, and code that runs once costs its instruction misses.  Up to 64 sequences
 // every wave does it for itself, and nothing goes through LDS.
 // Offsets that descend, or leave [0, T], would name rows twice or none: then there are no items at all.
-__device__ __forceinline__ Item find_item(const AttnArgs& a, int block, PlanShared& sh)
+template <bool TREE> __device__ __forceinline__ Item find_item(const AttnArgs& a, int block, PlanShared& sh)
 {
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int S = a.c.S, Hk = a.c.Hk;
@@ -100,7 +103,7 @@ __device__ __forceinline__ Item find_item(const AttnArgs& a, int block, PlanShar
         const int s = b + me;
         const int lo = a.c.off[s < S ? s : S], hi = a.c.off[s < S ? s + 1 : S], kv = a.c.lens[s < S ? s : S - 1];
         bad |= (lo < 0) | (hi < lo) | (hi > a.c.T);
-        q = shape_of(a, lo, bad ? lo : hi, kv);
+        q = shape_of<TREE>(a, lo, bad ? lo : hi, kv);
     };
     // the batch's work in tokens of a tile, of few rows and of many
     float few = 0, many = 0;
@@ -261,19 +264,22 @@ struct Range {
     int pieces;
     int begin, end;                 // tokens of the item's piece
 };
-__device__ __forceinline__ Range range_of(const AttnArgs& a, const Item& it)
+template <bool TREE> __device__ __forceinline__ Range range_of(const AttnArgs& a, const Item& it)
 {
     Range r;
+    const bool tree = is_tree<TREE>(a, it.q.n);
     r.rows = it.q.n * a.G;
     r.first = it.tile * it.q.units * 16;
     const int end = r.first + it.q.units * 16;
     const int last = (end < r.rows ? end : r.rows) - 1;
     r.p0 = it.q.kv - it.q.n;
     r.held = held_of(a.c, it.q.kv);
-    const int p_first = r.p0 + token_of(a, r.first), p_last = r.p0 + token_of(a, last);
+    // (a tree's rows stand anywhere from its root's position to its last row's, and all of them see what is cached before it)
+    const int p_first = tree ? r.p0 : r.p0 + token_of(a, r.first), p_last = tree ? it.q.kv - 1 : r.p0 + token_of(a, last);
     r.hi = a.causal && p_last + 1 < r.held ? p_last + 1 : r.held;
     if (r.hi < 0) r.hi = 0;
-    r.full_hi = a.causal && p_first + 1 < r.held ? p_first + 1 : r.held;
+    const int all_see = tree ? r.p0 : p_first + 1;
+    r.full_hi = a.causal && all_see < r.held ? all_see : r.held;
     r.lo = a.window > 0 && p_first - a.window + 1 > 0 ? p_first - a.window + 1 : 0;
     r.full_lo = a.window > 0 && p_last - a.window + 1 > 0 ? p_last - a.window + 1 : 0;
     r.lo &= ~31;
@@ -291,22 +297,73 @@ __device__ __forceinline__ Range range_of(const AttnArgs& a, const Item& it)
     return r;
 }
 
+// The first c of 64 bits.
+__device__ __forceinline__ uint64_t first_bits(int c) { return c <= 0 ? 0 : c >= 64 ? ~0ull : (1ull << c) - 1; }
+
+// The tokens that a row sees.
+template <bool TREE> struct Sight {
+    int lo, hi;                     // tokens [lo, hi)
+    __device__ __forceinline__ void step(const AttnArgs&, int) {}
+    __device__ __forceinline__ bool sees(int tok) const { return (tok < hi) & (tok >= lo); }
+};
+template <> struct Sight<true> {
+    int lo, hi;                     // tokens [lo, hi), and where `row` is not negative,
+    int row, p0, held;              // tokens p0 + j, before `held`, for the bits j of the row's mask
+    int t;
+    uint64_t bits;                  // bit i: token t + i
+    // Every row of a wave before the tokens t .. t + 63 are asked for: two words of the mask hold them.
+    __device__ __forceinline__ void step(const AttnArgs& a, int tok)
+    {
+        t = tok;
+        bits = first_bits(hi - t) & ~first_bits(lo - t);
+        const int at = t - p0;
+        if (row >= 0 && at > -64 && at < 64 * a.words) {
+            const uint64_t* m = a.masks + (int64_t)row * a.words;
+            uint64_t w;
+            if (at < 0) {
+                w = m[0] << -at;
+            } else {
+                const int i = at >> 6, r = at & 63;
+                w = m[i] >> r;
+                if (r > 0 && i + 1 < a.words) w |= m[i + 1] << (64 - r);
+            }
+            bits |= w & first_bits(held - t);
+        }
+    }
+    __device__ __forceinline__ bool sees(int tok) const { return ((bits >> (tok - t)) & 1) != 0; }
+};
+
 // What a packed row sees and where it lives.
-struct Row {
+template <bool TREE> struct Row {
     bool there;
     int row, head;                  // of the batch, of the queries
-    int see_lo, see_hi;             // tokens [see_lo, see_hi)
+    Sight<TREE> sight;
 };
-__device__ __forceinline__ Row row_of(const AttnArgs& a, const Item& it, const Range& rg, int r)
+template <bool TREE> __device__ __forceinline__ Row<TREE> row_of(const AttnArgs& a, const Item& it, const Range& rg, int r)
 {
-    Row x;
+    Row<TREE> x;
     x.there = r < rg.rows;
     const int tok = x.there ? token_of(a, r) : 0;
     x.row = it.q.row0 + tok;
     x.head = it.head * a.G + (x.there ? r - tok * a.G : 0);
     const int p = rg.p0 + tok;
-    x.see_hi = !x.there ? 0 : (a.causal && p + 1 < rg.held ? p + 1 : rg.held);
-    x.see_lo = a.window > 0 ? p - a.window + 1 : 0;
+    x.sight.hi = !x.there ? 0 : (a.causal && p + 1 < rg.held ? p + 1 : rg.held);
+    x.sight.lo = a.window > 0 ? p - a.window + 1 : 0;
+    if constexpr (TREE) {
+        if (x.sight.lo < 0) x.sight.lo = 0;      // (so that no difference of places leaves 32 bits)
+        x.sight.row = -1;
+        x.sight.p0 = rg.p0;
+        x.sight.held = rg.held;
+        if (is_tree<TREE>(a, it.q.n) && x.there) {
+            x.sight.row = x.row;
+            x.sight.hi = rg.p0 < rg.held ? rg.p0 : rg.held;
+            if (a.window > 0) {      // (a position is one of the sequence's rows', whatever the tensor holds)
+                const int at = a.positions[x.row], last = it.q.kv - 1;
+                const int lo = (at < rg.p0 ? rg.p0 : at > last ? last : at) - a.window + 1;
+                x.sight.lo = lo < 0 ? 0 : lo;
+            }
+        }
+    }
     return x;
 }
 
@@ -407,7 +464,7 @@ __device__ __forceinline__ float2 load_part_stats(const AttnArgs& a, int row)
 
 // Every thread of a block that has stored its piece of a tile calls it; the block that ends the tile joins its pieces, in their order (so
 // the result does not depend on who came last).  Sixteen lanes to a row, four pieces in flight.
-template <typename T, int DP, int UNITS>
+template <typename T, int DP, int UNITS, bool TREE>
 __device__ __forceinline__ void join_pieces(const AttnArgs& a, const Item& it, const Range& rg, int D, int32_t* flag)
 {
     if (!last_to_arrive(a.tickets + it.slot, (uint32_t)rg.pieces, flag)) return;
@@ -467,7 +524,7 @@ __device__ __forceinline__ void join_pieces(const AttnArgs& a, const Item& it, c
         }
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u) {
-            const Row row = row_of(a, it, rg, rg.first + (u0 + u) * 16 + q);
+            const auto row = row_of<TREE>(a, it, rg, rg.first + (u0 + u) * 16 + q);
             if (!row.there || u0 + u >= units) continue;
             const Finish f = finish_row(a, row.head, M[u], L[u]);
 #pragma unroll

@@ -41,7 +41,7 @@ template <int N> __device__ __forceinline__ void load_lds_group(const uint32_t (
                      "v"(off[2]), "v"(off[3]), "s"(base), "s"(lds), "n"(kGroupBias) : "memory");
 }
 
-template <bool FP8, int DP, bool EXACT> struct Many {
+template <bool FP8, int DP, bool EXACT, bool TREE> struct Many {
     static constexpr int TOK = 64;
     static constexpr int ROWB = DP * 2;              // bytes of a token's row in LDS
     static constexpr int CH = DP / 8;                // its 16-byte chunks
@@ -95,14 +95,14 @@ template <bool FP8, int DP, bool EXACT> struct Many {
 
     static __device__ __forceinline__ void run(const AttnArgs& a, const Item& it, char* smem)
     {
-        const Range rg = range_of(a, it);
+        const Range rg = range_of<TREE>(a, it);
         if (it.sub >= rg.pieces) return;
         const int lane = lane_id(), n = lane & 31, h = lane >> 5;
         const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
         const int D = EXACT ? DP : a.c.D, shift = a.c.page_shift, Hk = a.c.Hk;
         const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_address(smem));
 
-        const Row me = row_of(a, it, rg, rg.first + wave * 32 + n);
+        auto me = row_of<TREE>(a, it, rg, rg.first + wave * 32 + n);
         bf16x8_t qf[DP / 16];
         {
             const bf16_t* src = static_cast<const bf16_t*>(a.q) + (int64_t)me.row * a.ldq + (int64_t)me.head * D;
@@ -263,6 +263,7 @@ template <bool FP8, int DP, bool EXACT> struct Many {
             block_barrier();
             // a step whose tokens not every row sees
             const bool masked = cur.t + TOK > rg.full_hi || cur.t < rg.full_lo || cur.there != 0xffu;
+            if (masked) me.sight.step(a, cur.t);
             if (masked) clean_values(cur, rg, me, v_at, lds0 + at + HALF, smem, o);
             Step next{cur.t + TOK, 0};
             const bool more = next.t < rg.end;
@@ -292,7 +293,7 @@ template <bool FP8, int DP, bool EXACT> struct Many {
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {
                             const int grp = b * 4 + r / 4, tok = cur.t + grp * 8 + 4 * h + r % 4;
-                            const bool sees = (((cur.there >> grp) & 1) != 0) & (tok < me.see_hi) & (tok >= me.see_lo);
+                            const bool sees = (((cur.there >> grp) & 1) != 0) & me.sight.sees(tok);
                             s[b][r] = sees ? s[b][r] : -__builtin_inff();
                         }
                 }
@@ -372,7 +373,7 @@ template <bool FP8, int DP, bool EXACT> struct Many {
         for (int i = 0; i < 32 / RPI; ++i) {
             const int q = i * RPI + lane / OC;
             const float4 v = *reinterpret_cast<const float4*>(mine + q * DP * 4 + ((c ^ (q & (OC - 1))) * 16));
-            const Row row = row_of(a, it, rg, rg.first + wave * 32 + q);
+            const auto row = row_of<TREE>(a, it, rg, rg.first + wave * 32 + q);
             if (row.there && c * 4 < D) {
                 if (rg.pieces > 1) store_part(parts, part + q, c * 4, v);
                 else store_out<bf16_t>(a, row.row, row.head, D, c * 4, v);
@@ -380,14 +381,14 @@ template <bool FP8, int DP, bool EXACT> struct Many {
         }
         if (rg.pieces > 1) {
             __syncthreads();                                         // the flag shares the stages' memory
-            join_pieces<bf16_t, DP, 8>(a, it, rg, D, reinterpret_cast<int32_t*>(smem));
+            join_pieces<bf16_t, DP, 8, TREE>(a, it, rg, D, reinterpret_cast<int32_t*>(smem));
         }
     }
 
     // The values of a step whose tokens not every row sees, made fit for the second product, where a weight of zero keeps only finite
     // values out: tokens that are not there, or that no row sees, become zeros, whatever the cache holds; where there is an infinity or NaN
     // among the others, the rows that see it get it right away, and it becomes a zero too.  Every thread of the block calls it.
-    static __device__ __forceinline__ void clean_values(const Step& cur, const Range& rg, const Row& me, const uint32_t (&v_at)[2][NB],
+    static __device__ __forceinline__ void clean_values(const Step& cur, const Range& rg, const Row<TREE>& me, const uint32_t (&v_at)[2][NB],
                                                         uint32_t values, char* smem, float16_t (&o)[NB])
     {
         int32_t* flag = reinterpret_cast<int32_t*>(smem + 2 * STAGE);
@@ -418,7 +419,7 @@ template <bool FP8, int DP, bool EXACT> struct Many {
         });
         __syncthreads();
     }
-    static __device__ __forceinline__ void give_strange_values(const Step& cur, const Row& me, const uint32_t (&v_at)[2][NB], float16_t (&o)[NB])
+    static __device__ __forceinline__ void give_strange_values(const Step& cur, const Row<TREE>& me, const uint32_t (&v_at)[2][NB], float16_t (&o)[NB])
     {
         const int h = lane_id() >> 5;
 #pragma unroll
@@ -432,7 +433,7 @@ template <bool FP8, int DP, bool EXACT> struct Many {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int grp = 2 * k + i / 2, tok = cur.t + grp * 8 + 4 * h + (i % 2) * 2 + e;
-                        if (((cur.there >> grp) & 1) && tok < me.see_hi && tok >= me.see_lo) seen[i] |= 0x3f80u << (16 * e);
+                        if (((cur.there >> grp) & 1) && me.sight.sees(tok)) seen[i] |= 0x3f80u << (16 * e);
                     }
                 }
                 const uint4 v = __builtin_bit_cast(uint4, read_values(v_at, k, x));

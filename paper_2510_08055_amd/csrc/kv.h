@@ -42,6 +42,9 @@ struct AttnArgs {
     float* lse;
     const float* sinks;
     int64_t ldq, ldo;
+    const uint64_t* masks;         // of trees, [T, words]: bit j of row i: it sees row j of its sequence (words: 0 without trees)
+    const int32_t* positions;      // of their rows, read with a window alone
+    int words;
     int Hq, G, causal, window;
     int few_rows, tile_rows;       // packed rows of a tile, up to few_rows and where a sequence has more (set by the launch, as are:)
     int tile_tokens;               // tile_rows / G
@@ -56,5 +59,44 @@ struct AttnArgs {
 constexpr int kPartUnits = 8192;
 // clear_tickets: they are not known to be zero
 hipError_t launch_attention(int dtype, bool fp8, const AttnArgs& a, bool clear_tickets, hipStream_t s);
+// tree_attention.hip: the same with masks
+hipError_t launch_tree_attention(int dtype, bool fp8, const AttnArgs& a, bool clear_tickets, hipStream_t s);
+
+
+// kv_tree.hip
+constexpr int kMaxTreeWords = 16;      // of 64 rows each
+hipError_t launch_tree_masks(const KVView& c, const int32_t* parents, int words, int window, uint64_t* masks, int32_t* positions, hipStream_t s);
+
+// kv_weights.hip
+struct WeightArgs {
+    KVView c;
+    const void* q;
+    const float* lse;
+    float* scores;
+    int64_t ldq;
+    int Hq, G, causal, window;
+    uint32_t g_magic, hk_magic;    // (set by the launch)
+    float scale2, decay;
+};
+hipError_t launch_kv_weights(int dtype, bool fp8, const WeightArgs& a, hipStream_t s);
+
+// kv_select.hip
+struct SelectArgs {
+    KVView c;
+    const float* scores;
+    int32_t *keep, *keep_lens;
+    int budget, first, recent;
+};
+hipError_t launch_kv_select(const SelectArgs& a, hipStream_t s);
+
+// kv_compact.hip; row: bytes of a token's keys
+struct CompactArgs {
+    KVView c;
+    float* scores;
+    const int32_t *tokens, *lens, *first;
+    int64_t max_keep;
+    int per_head;
+};
+hipError_t launch_kv_compact(int row, const CompactArgs& a, hipStream_t s);
 
 }  // namespace moe
