@@ -87,7 +87,7 @@ struct SelectArgs {
     int32_t *keep, *keep_lens;
     int budget, first, recent;
 };
-hipError_t launch_kv_select(const SelectArgs& a, hipStream_t s);
+hipError_t launch_kv_select(const SelectArgs& a, void* workspace, size_t bytes, hipStream_t s);      // (the workspace need not be clear)
 
 // kv_compact.hip; row: bytes of a token's keys
 struct CompactArgs {

@@ -294,7 +294,7 @@ moe_status moe_kv_select(moe_kv_ctx* ctx, const float* scores, int64_t n_pages, 
     a.budget = opt->budget;
     a.first = opt->first;
     a.recent = opt->recent;
-    return dev(launch_kv_select(a, static_cast<hipStream_t>(stream)));
+    return dev(launch_kv_select(a, ctx->part, part_bytes(ctx->cfg), static_cast<hipStream_t>(stream)));
 }
 
 moe_status moe_kv_compact(moe_kv_ctx* ctx, const moe_kv_pages* pages, const moe_kv_batch* batch, const moe_kv_keep* keep, float* scores, void* stream)

@@ -143,20 +143,24 @@ def weights(b, lse, scores, causal=True, window=0, decay=1.0):
 
 
 def select(scores, lens, table, page, n_pages, budget, first, recent):
-    """keep [S, Hk, budget] and keep_lens [S]: a sort in Python."""
-    scores, table = scores.cpu(), table.cpu().tolist()
+    """keep [S, Hk, budget] and keep_lens [S], by a sort of each sequence and head."""
+    scores, table = scores.cpu(), table.cpu().long()
     S, hk = len(lens), scores.shape[1]
     keep, kept = torch.full((S, hk, budget), -1, dtype=torch.int32), torch.zeros(S, dtype=torch.int32)
     for s, kv in enumerate(lens):
-        held = min(max(kv, 0), len(table[s]) * page)
-        there = [j for j in range(held) if 0 <= table[s][j // page] < n_pages]
-        kept[s] = min(budget, len(there))
+        held = min(max(kv, 0), table.shape[1] * page)
+        j = torch.arange(held)
+        ids = table[s][j // page]
+        j = j[(ids >= 0) & (ids < n_pages)]
+        kept[s] = n = min(budget, len(j))
         for h in range(hk):
-            def key(j):
-                x = float(scores[table[s][j // page], h, j % page])
-                sure = j < first or j >= kv - recent
-                return (not sure, math.inf if x != x or x == -math.inf else -x if x != 0 else 0.0, j)
-            keep[s, h, :kept[s]] = torch.tensor(sorted(sorted(there, key=key)[:budget]), dtype=torch.int32)
+            x = scores[table[s][j // page], h, j % page].double()
+            x = torch.where(torch.isnan(x), -math.inf, x) + 0.0
+            sure = (j < first) | (j >= kv - recent)
+            # kept for sure before all others, then the larger score, then the lower token: sorts that keep the order of equals
+            order = torch.argsort(-x, stable=True)
+            order = order[torch.argsort((~sure[order]).int(), stable=True)]
+            keep[s, h, :n] = j[order[:n]].sort().values.int()
     return keep, kept
 
 

@@ -161,6 +161,16 @@ def test_select_of_long_sequences(gpu_lib, kv, budget):
     check_select(gpu_lib, kv, 64, 2, budget, 1 if budget > 1 else 0, 0)
 
 
+@pytest.mark.parametrize("kv", [[30000, 5, 16384, 16385, 0, 24577], [100000, 3000]])
+@pytest.mark.parametrize("budget,first,recent", [(1, 0, 0), (2000, 4, 256), (16384, 0, 16000), (24576, 100, 100), (99999, 0, 0), (100000, 1, 1)])
+def test_select_of_parts(gpu_lib, kv, budget, first, recent):
+    """Sequences that several blocks share beside ones that a block has alone; holes, equal scores, two values."""
+    check_select(gpu_lib, kv, 32, 1, budget, first, recent)
+    check_select(gpu_lib, kv, 32, 2, budget, first, recent, dropped=[(0, i) for i in range(0, 900, 7)], seed=2)
+    check_select(gpu_lib, kv, 32, 1, budget, first, recent, make=lambda x: torch.zeros_like(x))
+    check_select(gpu_lib, kv, 32, 1, budget, first, recent, make=lambda x: (x > 1).float())
+
+
 @pytest.mark.parametrize("values", [[0.0], [0.0, -0.0], [1.0, 0.0], [1.0, math.nan, -math.inf, -2.0], [math.inf, -math.inf, math.nan, 0.0, 3.5],
                                     [1e-45, 0.0, -1e-45, 1e-38], [1.0, 1.0 + 2.0 ** -23, 1.0 - 2.0 ** -24], [3.4e38, math.inf], [math.nan], [-math.inf, math.nan]])
 def test_select_of_equal_and_strange_scores(gpu_lib, values):
