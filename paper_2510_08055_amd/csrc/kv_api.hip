@@ -108,6 +108,22 @@ moe_status view_of_tokens(const moe_kv_ctx* ctx, int64_t n_pages, const moe_kv_b
 
 inline float scale2_of(const moe_kv_config& g) { return (float)(1.4426950408889634 / std::sqrt((double)g.dim)); }
 
+// A launch that uses the tickets.  They are zero between launches once they have been cleared: in front of a context's first call.  A call that is
+// being captured carries the clear along, runs when its graph is replayed, and so leaves it to the next call as well.
+template <typename F> moe_status with_tickets(moe_kv_ctx* ctx, void* stream, F launch)
+{
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const bool clear = !ctx->tickets_clear;
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (clear && hipStreamIsCapturing(s, &capture) != hipSuccess) {
+        (void)hipGetLastError();        // (the legacy stream while another one is captured)
+        capture = hipStreamCaptureStatusActive;
+    }
+    const moe_status st = dev(launch(clear, s));
+    if (clear) ctx->tickets_clear = st == MOE_OK && capture == hipStreamCaptureStatusNone;
+    return st;
+}
+
 // Attention, of rows as they follow each other or (tree) of trees.
 moe_status attend(moe_kv_ctx* ctx, const void* q, int64_t ldq, int64_t T, const moe_kv_pages* pages, const moe_kv_batch* batch, const moe_tree* tree,
                   const moe_attention_options* opt, void* out, int64_t ldo, float* lse, void* stream)
@@ -141,18 +157,9 @@ moe_status attend(moe_kv_ctx* ctx, const void* q, int64_t ldq, int64_t T, const 
     a.part = ctx->part;
     a.part_stats = ctx->part_stats;
     a.tickets = ctx->tickets;
-    const hipStream_t s = static_cast<hipStream_t>(stream);
-    // The tickets are zero between launches once they have been cleared: in front of a context's first call.  A call that is
-    // being captured carries the clear along, runs when its graph is replayed, and so leaves it to the next call as well.
-    const bool clear = !ctx->tickets_clear;
-    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-    if (clear && hipStreamIsCapturing(s, &capture) != hipSuccess) {
-        (void)hipGetLastError();        // (the legacy stream while another one is captured)
-        capture = hipStreamCaptureStatusActive;
-    }
-    st = dev(tree ? launch_tree_attention(g.dtype, g.kv_format == MOE_KV_FP8, a, clear, s) : launch_attention(g.dtype, g.kv_format == MOE_KV_FP8, a, clear, s));
-    if (clear) ctx->tickets_clear = st == MOE_OK && capture == hipStreamCaptureStatusNone;
-    return st;
+    return with_tickets(ctx, stream, [&](bool clear, hipStream_t s) {
+        return tree ? launch_tree_attention(g.dtype, g.kv_format == MOE_KV_FP8, a, clear, s) : launch_attention(g.dtype, g.kv_format == MOE_KV_FP8, a, clear, s);
+    });
 }
 
 }  // namespace
@@ -274,7 +281,9 @@ moe_status moe_kv_weights(moe_kv_ctx* ctx, const void* q, int64_t ldq, const flo
     a.window = opt->window;
     a.scale2 = scale2_of(g);
     a.decay = opt->decay;
-    return dev(launch_kv_weights(g.dtype, g.kv_format == MOE_KV_FP8, a, static_cast<hipStream_t>(stream)));
+    a.part = ctx->part;
+    a.tickets = ctx->tickets;
+    return with_tickets(ctx, stream, [&](bool clear, hipStream_t s) { return launch_kv_weights(g.dtype, g.kv_format == MOE_KV_FP8, a, clear, s); });
 }
 
 moe_status moe_kv_select(moe_kv_ctx* ctx, const float* scores, int64_t n_pages, const moe_kv_batch* batch, const moe_select_options* opt,

@@ -1,249 +1,659 @@
 // The attention weight that cached tokens receive: column sums of exp(q . k / sqrt(dim) - lse), without the matrix they are sums of.
 //
-// Scores are computed transposed as in the attention, S = K Q^T, but here the keys stay and the rows pass by: a block holds 64 tokens' keys
-// as the first operand, its four waves take 32 packed rows in turn, and a lane adds up the exponentials of its column's rows for the 16 tokens of each
-// output tile that it holds.  Every token's sum belongs to one block: there are no atomics, and the order is fixed.
-#include <cfloat>
-
-#include "kv.h"
+// Scores are computed transposed as in the attention, S = K Q^T, a query row to a lane's column: a row's lse is lane-local, and the sums of the
+// exponentials over the rows stay in the lanes until the end.  There are two bodies: for sequences of few rows the rows stay in registers and the keys
+// stream by (read once: that bounds it); for many rows the keys of 64 tokens stay in a wave's registers and the rows pass by.
+//
+// Work is cut on the device, from the descriptors, into equal stretches: of 32-token units of all sequences and heads, a stretch to a wave, where rows are
+// few; where they are many, of steps (64 packed rows by 256 tokens), a stretch to a block.  A token's sum belongs to one wave, or is joined from the
+// stretches that its tokens' steps fall into, in their order, by the block that ends the last: there are no atomic sums, and a batch's result is always the same bits.
+#include "attention_plan.h"
 
 namespace moe {
 namespace {
 
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef float float16_t __attribute__((ext_vector_type(16)));
+constexpr int kSeqs = 256;             // sequences that are planned at a time, a thread each
+constexpr int kFewRows = 16;           // packed rows of a sequence up to which they stay in registers
+constexpr int kMinSteps = 8;           // of a stretch, where there are too few for all blocks
 
-constexpr float kLog2e = 1.44269504088896340736f;
+__device__ __forceinline__ int token_of(const WeightArgs& a, int r) { return a.G == 1 ? r : (int)divided((uint32_t)r, (uint32_t)a.G, a.g_magic); }
 
-__device__ __forceinline__ uint32_t divided(uint32_t v, uint32_t d, uint32_t magic)
+struct WeightSeq {
+    int row0, n, p0, held;             // p0: the position of the first row; held: 0 where no score changes
+    int lo;                            // the first token whose score changes
+};
+__device__ __forceinline__ WeightSeq seq_of(const WeightArgs& a, int s)
 {
-    const uint32_t q = __umulhi(v, magic);
-    return q * d > v ? q - 1 : q;
+    WeightSeq q;
+    q.row0 = a.c.off[s];
+    const int hi = a.c.off[s + 1], kv = a.c.lens[s] > 0 ? a.c.lens[s] : 0;
+    q.n = q.row0 < 0 || hi < q.row0 || hi > a.c.T ? 0 : hi - q.row0;
+    q.held = q.n > 0 ? held_of(a.c, kv) : 0;
+    q.p0 = kv - q.n;
+    const int first = q.p0 - a.window + 1;
+    q.lo = a.window > 0 && a.decay == 1.0f && first > 0 ? first : 0;      // (what no row sees stays as it is)
+    if (q.lo >= q.held) q.held = 0;
+    return q;
 }
 
-struct Shared {
-    int first[256];                // items of the chunk's sequences up to and with each
-    int sums[4];
-    float w[4][64];
-};
+// The index of a token's score, -1 where it is not there.
+__device__ __forceinline__ int64_t place_of(const WeightArgs& a, const WeightSeq& q, int seq, int h, int j)
+{
+    const int id = j >= q.lo && j < q.held ? a.c.table[(int64_t)seq * a.c.max_pages + (j >> a.c.page_shift)] : -1;
+    return id < 0 || id >= a.c.n_pages ? -1 : page_row(id, a.c.Hk, h, a.c.page_shift, j & ((1 << a.c.page_shift) - 1));
+}
 
-template <typename T, bool FP8, int DP> struct Weights {
+// A row's lse as a power of two; infinity where the row adds nothing.
+__device__ __forceinline__ float lse2_of(const WeightArgs& a, int64_t row, int head)
+{
+    const float v = a.lse[row * a.Hq + head];
+    return v == -__builtin_inff() ? __builtin_inff() : v * kLog2e;
+}
+
+__device__ __forceinline__ void store_score(const WeightArgs& a, const WeightSeq& q, int64_t at, int j, float w)
+{
+    if (j < q.p0 && a.decay != 0.0f) w += a.decay * a.scores[at];
+    a.scores[at] = w;
+}
+
+// ---- few rows ----
+template <typename T, bool FP8, int DP> struct FewWeights {
     static constexpr bool F32 = sizeof(T) == 4;
-    static constexpr int TOK = F32 && DP > 128 ? 32 : 64, NB = TOK / 32;
-    static constexpr int CD = F32 ? 8 : 16, KC = DP / CD, LD = CD / 2;      // dimensions of a step of the product, steps, dimensions of a lane in it
+    static constexpr int NJ = F32 ? 1 : 2, TOK = NJ * 16;          // 16-token subtiles of a step
+    static constexpr int ESZ = FP8 ? 1 : (int)sizeof(T);
+    static constexpr int KC = DP / (F32 ? 16 : (FP8 ? 64 : 32));   // key loads per subtile
+    static constexpr int KDIM = F32 ? 4 : (FP8 ? 16 : 8);          // dimensions of such a load
+    static constexpr int KDW = KDIM * ESZ / 4;
 
-    struct Seq {
-        int row0, n, kv, held, lo;      // lo: the first token whose score changes
+    static __device__ __forceinline__ int units(const WeightSeq& q) { return q.held > 0 ? (q.held - (q.lo & ~(TOK - 1)) + TOK - 1) / TOK : 0; }
+
+    struct Queries {
+        bf16x8_t b[F32 ? 1 : DP / 32];
+        float f[F32 ? DP / 16 : 1][4];
+        float lse2;
+        int see_lo, see_hi;
     };
-    static __device__ __forceinline__ Seq seq_of(const WeightArgs& a, int s)
+    static __device__ __forceinline__ Queries queries_of(const WeightArgs& a, const WeightSeq& q, int h, int r)
     {
-        Seq q;
-        q.row0 = a.c.off[s];
-        const int hi = a.c.off[s + 1];
-        q.n = q.row0 < 0 || hi < q.row0 || hi > a.c.T ? 0 : hi - q.row0;
-        q.kv = a.c.lens[s] > 0 ? a.c.lens[s] : 0;
-        const int most = a.c.max_pages << a.c.page_shift;
-        q.held = q.n > 0 ? (q.kv < most ? q.kv : most) : 0;
-        q.lo = 0;
-        if (a.window > 0 && a.decay == 1.0f) {
-            const int first = q.kv - q.n - a.window + 1;
-            q.lo = first > 0 ? first & ~(TOK - 1) : 0;
+        Queries Q;
+        const int g = lane_id() >> 4, D = a.c.D;
+        const bool there = r < q.n * a.G;
+        const int tok = there ? token_of(a, r) : 0, head = h * a.G + (there ? r - tok * a.G : 0);
+        const int64_t row = q.row0 + tok;
+        const T* src = static_cast<const T*>(a.q) + row * a.ldq + (int64_t)head * D;
+        Q.lse2 = lse2_of(a, row, head);
+        const int p = q.p0 + tok;
+        Q.see_hi = !there || Q.lse2 == __builtin_inff() ? 0 : a.causal ? p + 1 : 0x7fffffff;
+        Q.see_lo = a.window > 0 ? p - a.window + 1 : 0;
+        if constexpr (F32) {
+#pragma unroll
+            for (int c = 0; c < DP / 16; ++c) {
+                const int d = c * 16 + g * 4;
+                const float4 v = *reinterpret_cast<const float4*>(src + (d < D ? d : 0));
+                const bool in = d < D;
+                Q.f[c][0] = in ? v.x : 0; Q.f[c][1] = in ? v.y : 0; Q.f[c][2] = in ? v.z : 0; Q.f[c][3] = in ? v.w : 0;
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < DP / 32; ++c) {
+                const int d = FP8 ? (c / 2) * 64 + g * 16 + (c % 2) * 8 : c * 32 + g * 8;
+                uint4 v = *reinterpret_cast<const uint4*>(src + (d < D ? d : 0));
+                if (d >= D) v = make_uint4(0, 0, 0, 0);
+                Q.b[c] = __builtin_bit_cast(bf16x8_t, v);
+            }
         }
-        return q;
+        return Q;
     }
 
-    static __device__ void item(const WeightArgs& a, const Seq& q, int seq, int h, int j0, Shared& sh)
+    // Tokens [begin, end) of a sequence and head, begin a multiple of TOK; a wave's.
+    static __device__ __forceinline__ void run(const WeightArgs& a, const WeightSeq& q, int seq, int h, int begin, int end)
     {
-        const int lane = lane_id(), n = lane & 31, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-        const int D = a.c.D, shift = a.c.page_shift, G = a.G;
-        auto place = [&](int j) -> int64_t {
-            const int p = j >> shift;
-            const int id = j < q.held ? a.c.table[(int64_t)seq * a.c.max_pages + p] : -1;
-            return id < 0 || id >= a.c.n_pages ? -1 : page_row(id, a.c.Hk, h, shift, j & ((1 << shift) - 1));
+        const int lane = lane_id(), n = lane & 15, g = lane >> 4, D = a.c.D, shift = a.c.page_shift;
+        Entries pages;
+        pages.hold(a.c, seq, begin >> shift, end);
+        const int rows = q.n * a.G;
+        Queries Q = queries_of(a, q, h, n);
+
+        auto page_of = [&](int t) { return __shfl(pages.id, (t >> shift) - pages.base); };
+        auto slot_of = [&](int id, int t) { return page_row(id < 0 ? 0 : id, a.c.Hk, h, shift, t & ((1 << shift) - 1)); };
+        // a step's loads: keys of token 16 j + n; the score that this lane will store, of token 16 (n / 4) + 4 g + n % 4
+        struct Step {
+            uint32_t k[NJ][KC][KDW];
+            uint32_t scale[NJ];
+            int64_t at;
+            float old;
         };
-        bf16x8_t kb[F32 ? 1 : NB][F32 ? 1 : KC];
-        float kf[F32 ? NB : 1][F32 ? KC : 1][4];
+        const int mine = (n >> 2) * 16 + 4 * g + (n & 3);
+        auto load = [&](int t) {
+            Step x;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const int tok = t + j * 16 + n;
+                const int64_t row = slot_of(page_of(tok), tok);
+                const char* p = a.c.k + row * D * ESZ;
+#pragma unroll
+                for (int c = 0; c < KC; ++c) {
+                    const int d = c * (4 * KDIM) + g * KDIM;
+                    load_dwords<true>(p + (d < D ? d : 0) * ESZ, x.k[j][c]);
+                }
+                if constexpr (FP8) x.scale[j] = a.c.ks[row];
+            }
+            const int tok = t + mine, id = page_of(n < 4 * NJ ? tok : t);
+            x.at = n < 4 * NJ && id >= 0 && tok >= q.lo && tok < end ? slot_of(id, tok) : -1;
+            x.old = 0;
+            if (x.at >= 0 && tok < q.p0 && a.decay != 0.0f) x.old = a.scores[x.at];
+            return x;
+        };
+        Step x = load(begin);
+        for (int t = begin; t < end; t += TOK) {
+            const bool more = t + TOK < end;
+            if (more && ((t + 2 * TOK - 1) >> shift) - pages.base >= 64) pages.hold(a.c, seq, (t + TOK) >> shift, end);
+            Step next;
+            if (more) next = load(t + TOK);
+            // the keys as the first product's operand
+            bf16x8_t kb[F32 ? 1 : NJ][F32 ? 1 : DP / 32];
+            float kf[F32 ? DP / 16 : 1][4];
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                float sc = 1.0f;
+                if constexpr (FP8) sc = scale_of(x.scale[j]);
+#pragma unroll
+                for (int c = 0; c < KC; ++c) {
+                    // (past the dimension the keys are zeros, like the queries: an infinity times zero would be NaN)
+                    const bool in = c * (4 * KDIM) + g * KDIM < D;
+                    uint32_t w[KDW];
+#pragma unroll
+                    for (int i = 0; i < KDW; ++i) w[i] = in ? x.k[j][c][i] : 0;
+                    if constexpr (F32 && FP8) {
+                        const hw_float2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[0], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[0], true);
+                        kf[c][0] = lo[0] * sc; kf[c][1] = lo[1] * sc; kf[c][2] = hi[0] * sc; kf[c][3] = hi[1] * sc;
+                    } else if constexpr (F32) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) kf[c][i] = __uint_as_float(w[i]);
+                    } else if constexpr (FP8) {      // exact: a code has 4 significant bits, its scale is a power of two
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const bf16x2_t lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], sc, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], sc, true);
+                            bf16x8_t& to = kb[j][c * 2 + i / 2];
+                            to[(i % 2) * 4] = lo[0]; to[(i % 2) * 4 + 1] = lo[1]; to[(i % 2) * 4 + 2] = hi[0]; to[(i % 2) * 4 + 3] = hi[1];
+                        }
+                    } else {
+                        kb[j][c] = __builtin_bit_cast(bf16x8_t, x.k[j][c]);
+                        if (!in) kb[j][c] = bf16x8_t{};
+                    }
+                }
+            }
+            float sum[NJ][4] = {};
+            for (int r0 = 0;;) {
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    float4_t s = float4_t{0, 0, 0, 0};
+                    if constexpr (F32) {
+#pragma unroll
+                        for (int c = 0; c < DP / 16; ++c)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[c][i], Q.f[c][i], s, 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < DP / 32; ++c) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb[j][c], Q.b[c], s, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int tok = t + j * 16 + 4 * g + r;
+                        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.scale2, -Q.lse2));
+                        sum[j][r] += ((tok < Q.see_hi) & (tok >= Q.see_lo)) ? w : 0.0f;
+                    }
+                }
+                r0 += 16;
+                if (r0 >= rows) break;      // (more than 16 rows: in batches of few rows alone, and rare)
+                Q = queries_of(a, q, h, r0 + n);
+            }
+            if (rows > 16) Q = queries_of(a, q, h, n);
+            // over the sixteen columns; lane n keeps the sum of its token
+            float w = 0;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float v = sum[j][r];
+                    auto turn = [&](auto ctrl) {
+                        v += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), decltype(ctrl)::value, 0xF, 0xF, true));
+                    };
+                    using std::integral_constant;
+                    turn(integral_constant<int, 0x128>{});      // from 8, 4, 2 and 1 lanes around the sixteen
+                    turn(integral_constant<int, 0x124>{});
+                    turn(integral_constant<int, 0x122>{});
+                    turn(integral_constant<int, 0x121>{});
+                    w = n == j * 4 + r ? v : w;
+                }
+            if (x.at >= 0) a.scores[x.at] = __builtin_fmaf(a.decay, x.old, w);
+            if (more) x = next;
+        }
+    }
+};
+
+// ---- many rows ----
+// The steps of a sequence and head: tiles of TOK tokens, of each of which the rows that see it are taken ROWS at a time.  Tiles start at the
+// position of the first row, or a whole number of tiles from it, so that the rows a causal mask leaves out are whole steps.
+struct Steps {
+    int first, end;                    // tiles
+    int t0;                            // the tile that starts at p0
+    int total;                         // steps that hold all rows
+    int less;                          // by which each tile from t0 on has its rows start later (causal)
+    int each;                          // steps of a tile, where they are the same for all; 0: all rows from the first that sees it
+};
+template <typename T, bool FP8, int DP> struct ManyWeights {
+    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr int NB = F32 && DP > 128 ? 1 : 2, WTOK = 32 * NB, TOK = 4 * WTOK;      // tokens of a wave, of a block
+    static constexpr int ROWS = F32 ? 32 : 64;
+    static constexpr int CD = F32 ? 8 : 16, KC = DP / CD, LD = CD / 2;      // dimensions of a step of the product, steps, dimensions of a lane in it
+    static constexpr int ROWB = DP * (int)sizeof(T), CH = ROWB / 16;        // bytes of a row in LDS, its 16-byte chunks
+    static constexpr int LOADS = ROWS * CH / 256;
+    static constexpr int STAGE = ROWS * ROWB;
+    static constexpr size_t LDS = 2 * STAGE + 2 * ROWS * 4 + TOK * 4 + 16;  // rows, their lse, a tile's sums, a flag
+
+    static __device__ __forceinline__ Steps steps_of(const WeightArgs& a, const WeightSeq& q)
+    {
+        Steps s{0, 0, 0, 0, 0, 0};
+        if (q.held == 0) return s;
+        s.total = (int)(((int64_t)q.n * a.G + ROWS - 1) / ROWS);
+        s.t0 = q.p0 > 0 ? (q.p0 + TOK - 1) / TOK : 0;
+        const int64_t start = q.p0 - (int64_t)s.t0 * TOK;      // of tile 0: at most 0
+        s.end = (int)((q.held - start + TOK - 1) / TOK);
+        s.first = (int)((q.lo - start) / TOK);
+        s.less = a.causal ? TOK / ROWS * a.G : 0;
+        const int64_t band = a.causal && a.window > 0 ? (((int64_t)TOK + a.window) * a.G + ROWS - 1) / ROWS + 1 : s.total;
+        s.each = !a.causal || band < s.total ? (int)band : 0;
+        return s;
+    }
+    // steps of the tiles before t
+    static __device__ __forceinline__ int64_t before(const Steps& s, int t)
+    {
+        if (s.each > 0) return (int64_t)(t - s.first) * s.each;
+        const int64_t m = t > s.t0 ? t - (s.first > s.t0 ? s.first : s.t0) : 0, skip = s.first > s.t0 ? s.first - s.t0 : 0;
+        const int64_t whole = (t < s.t0 ? t : s.t0) - s.first;
+        return (whole > 0 ? whole * s.total : 0) + m * s.total - s.less * (m * (m - 1) / 2 + m * skip);
+    }
+
+    static __device__ __forceinline__ int swz(int r)
+    {
+        if constexpr (ROWB == 128) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+        else return ((r & 3) << 2) | ((r >> 2) & 3);
+    }
+
+    struct Keys {
+        bf16x8_t b[F32 ? 1 : NB][F32 ? 1 : KC];
+        float f[F32 ? NB : 1][F32 ? KC : 1][4];
+    };
+    static __device__ __forceinline__ void load_keys(const WeightArgs& a, const WeightSeq& q, int seq, int h, int j0, Keys& K)
+    {
+        const int lane = lane_id(), n = lane & 31, half = lane >> 5, D = a.c.D;
+        int64_t row[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) row[b] = place_of(a, q, seq, h, j0 + b * 32 + n);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            const int64_t at = place(j0 + b * 32 + n), row = at < 0 ? 0 : at;       // (a token that is not there: some row, its sum is not stored)
+            if (row[b] < 0) row[b] = 0;          // (a token that is not there: some row, its sum is not stored)
             float sc = 1.0f;
-            if constexpr (FP8) sc = scale_of(a.c.ks[row]);
+            if constexpr (FP8) sc = scale_of(a.c.ks[row[b]]);
 #pragma unroll
             for (int c = 0; c < KC; ++c) {
                 const int d = c * CD + half * LD;
-                const char* p = a.c.k + (row * D + (d < D ? d : 0)) * (FP8 ? 1 : (int)sizeof(T));
+                const bool in = d < D;           // (past the dimension: zeros, like the rows)
+                const char* p = a.c.k + (row[b] * D + (in ? d : 0)) * (FP8 ? 1 : (int)sizeof(T));
                 if constexpr (F32) {
+                    float4 v;
                     if constexpr (FP8) {
                         const int u = *reinterpret_cast<const int*>(p);
                         const hw_float2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8(u, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(u, true);
-                        kf[b][c][0] = lo[0] * sc; kf[b][c][1] = lo[1] * sc; kf[b][c][2] = hi[0] * sc; kf[b][c][3] = hi[1] * sc;
+                        v = make_float4(lo[0] * sc, lo[1] * sc, hi[0] * sc, hi[1] * sc);
                     } else {
-                        const float4 v = *reinterpret_cast<const float4*>(p);
-                        kf[b][c][0] = v.x; kf[b][c][1] = v.y; kf[b][c][2] = v.z; kf[b][c][3] = v.w;
+                        v = *reinterpret_cast<const float4*>(p);
                     }
-                } else if constexpr (FP8) {      // exact: a code has 4 significant bits, its scale is a power of two
+                    K.f[b][c][0] = in ? v.x : 0; K.f[b][c][1] = in ? v.y : 0; K.f[b][c][2] = in ? v.z : 0; K.f[b][c][3] = in ? v.w : 0;
+                } else if constexpr (FP8) {
                     const uint2 u = *reinterpret_cast<const uint2*>(p);
-                    const uint32_t w[2] = {u.x, u.y};
+                    const uint32_t w[2] = {in ? u.x : 0, in ? u.y : 0};
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const bf16x2_t lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], sc, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], sc, true);
-                        kb[b][c][4 * i] = lo[0]; kb[b][c][4 * i + 1] = lo[1]; kb[b][c][4 * i + 2] = hi[0]; kb[b][c][4 * i + 3] = hi[1];
+                        K.b[b][c][4 * i] = lo[0]; K.b[b][c][4 * i + 1] = lo[1]; K.b[b][c][4 * i + 2] = hi[0]; K.b[b][c][4 * i + 3] = hi[1];
                     }
                 } else {
-                    kb[b][c] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(p));
+                    uint4 v = *reinterpret_cast<const uint4*>(p);
+                    if (!in) v = make_uint4(0, 0, 0, 0);
+                    K.b[b][c] = __builtin_bit_cast(bf16x8_t, v);
                 }
             }
         }
+    }
+
+    // Steps [x0, x1) of a tile's `count`, as piece `piece` of `pieces`; slot: where piece 0 leaves its sums, and its ticket.
+    static __device__ __forceinline__ void run(const WeightArgs& a, const WeightSeq& q, const Steps& st, int seq, int h, int tile, int x0, int x1, int piece,
+                                               int pieces, int slot, char* smem)
+    {
+        const int tid = threadIdx.x, lane = lane_id(), n = lane & 31, half = lane >> 5;
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int D = a.c.D, rows = q.n * a.G;
+        float* const lse = reinterpret_cast<float*>(smem + 2 * STAGE);
+        float* const sums = lse + 2 * ROWS;
+        int32_t* const flag = reinterpret_cast<int32_t*>(sums + TOK);
+        const int start = (int)(q.p0 + ((int64_t)tile - st.t0) * TOK);         // (from -TOK on)
+        const int j0 = start + wave * WTOK, j1 = j0 + WTOK - 1;
+        const int skip = tile > st.t0 ? (tile - st.t0) * st.less : 0;          // steps whose rows do not see the tile
+        int r0 = (int64_t)(skip + x0) * ROWS < rows ? (skip + x0) * ROWS : rows;
+        const int r1 = (int64_t)(skip + x1) * ROWS < rows ? (skip + x1) * ROWS : rows;
+
+        Keys K;
+        load_keys(a, q, seq, h, j0, K);
+
+        // a stage's rows: 16 bytes to a thread and load
+        uint4 raw[LOADS];
+        float raw_lse = 0;
+        auto row_at = [&](int r, int64_t& row, int& head) {
+            const int rr = r < rows ? r : rows - 1, tok = token_of(a, rr);
+            row = q.row0 + tok;
+            head = h * a.G + rr - tok * a.G;
+        };
+        auto fetch = [&](int from) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int at = i * 256 + tid, chunk = at % CH;
+                int64_t row;
+                int head;
+                row_at(from + at / CH, row, head);
+                const char* src = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + row * a.ldq + (int64_t)head * D);
+                const bool in = chunk * 16 < D * (int)sizeof(T);
+                raw[i] = *reinterpret_cast<const uint4*>(src + (in ? chunk * 16 : 0));
+                if (!in) raw[i] = make_uint4(0, 0, 0, 0);
+            }
+            if (tid < ROWS) {
+                int64_t row;
+                int head;
+                row_at(from + tid, row, head);
+                raw_lse = from + tid < rows ? lse2_of(a, row, head) : __builtin_inff();
+            }
+        };
+        auto put = [&](int stage) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int at = i * 256 + tid, r = at / CH, chunk = at % CH;
+                *reinterpret_cast<uint4*>(smem + stage * STAGE + r * ROWB + ((chunk ^ swz(r)) * 16)) = raw[i];
+            }
+            if (tid < ROWS) lse[stage * ROWS + tid] = raw_lse;
+        };
+
         float acc[NB][16];
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[b][r] = 0;
+            for (int i = 0; i < 16; ++i) acc[b][i] = 0;
+        if (r0 < r1) {
+            fetch(r0);
+            put(0);
+        }
+        int stage = 0;
+        for (; r0 < r1; r0 += ROWS, stage ^= 1) {
+            __syncthreads();
+            const bool more = r0 + ROWS < r1;
+            if (more) fetch(r0 + ROWS);
+#pragma unroll 1
+            for (int part = 0; part < ROWS / 32; ++part) {
+                const int first = r0 + part * 32;
+                if (first >= rows) break;
+                const int last = first + 31 < rows ? first + 31 : rows - 1;
+                const int p_first = q.p0 + token_of(a, first), p_last = q.p0 + token_of(a, last);
+                if ((a.causal && p_last < j0) || (a.window > 0 && p_first - a.window + 1 > j1)) continue;      // none of the rows sees a token of the wave
+                const char* at = smem + stage * STAGE + (part * 32 + n) * ROWB;
+                const float l2 = lse[stage * ROWS + part * 32 + n];
+                float16_t s[NB];
+#pragma unroll
+                for (int b = 0; b < NB; ++b) s[b] = float16_t{};
+#pragma unroll
+                for (int c = 0; c < KC; ++c) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(at + (((2 * c + half) ^ swz(n)) * 16));
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        if constexpr (F32) {
+                            const float f[4] = {__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)};
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) s[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(K.f[b][c][i], f[i], s[b], 0, 0, 0);
+                        } else {
+                            s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(K.b[b][c], __builtin_bit_cast(bf16x8_t, v), s[b], 0, 0, 0);
+                        }
+                    }
+                }
+                const bool masked = (a.causal && p_first < j1) || (a.window > 0 && p_last - a.window + 1 > j0) || __any(l2 == __builtin_inff());
+                if (!masked) {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[b][i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], a.scale2, -l2));
+                } else {
+                    const int p = q.p0 + token_of(a, first + n < rows ? first + n : rows - 1);
+                    const int see_hi = l2 == __builtin_inff() ? start : a.causal ? p + 1 : 0x7fffffff, see_lo = a.window > 0 ? p - a.window + 1 : -0x7fffffff;
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int j = j0 + b * 32 + (i / 4) * 8 + 4 * half + i % 4;
+                            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], a.scale2, -l2));
+                            acc[b][i] += ((j < see_hi) & (j >= see_lo)) ? w : 0.0f;
+                        }
+                }
+            }
+            if (more) put(stage ^ 1);
+        }
 
-        // the rows that see some of the tokens, as packed rows; tiles of 32
-        const int p0 = q.kv - q.n;
-        int t_lo = a.causal && j0 > p0 ? j0 - p0 : 0, t_hi = q.n;
-        if (a.window > 0) {
-            const int64_t end = (int64_t)j0 + TOK - 1 - p0 + a.window;
-            t_hi = end < t_hi ? (int)end : t_hi;
-        }
-        const int rows = q.n * G, end = t_hi * G;
-        for (int r0 = (t_lo * G / 32 + wave) * 32; r0 < end; r0 += 128) {
-            const int r = r0 + n;
-            const bool there = r < rows;
-            const int tok = !there ? 0 : G == 1 ? r : (int)divided((uint32_t)r, (uint32_t)G, a.g_magic);
-            const int head = h * G + (there ? r - tok * G : 0);
-            const int64_t row = q.row0 + tok;
-            const float lse = a.lse[row * a.Hq + head];
-            const T* src = static_cast<const T*>(a.q) + row * a.ldq + (int64_t)head * D;
-            float16_t s[NB];
+        // over the 32 columns: halves of the sums change sides with half of the lanes, until a lane has one
 #pragma unroll
-            for (int b = 0; b < NB; ++b) s[b] = float16_t{};
+        for (int b = 0; b < NB; ++b) {
+            float v[16];
 #pragma unroll
-            for (int c = 0; c < KC; ++c) {
-                if (c * CD >= D) break;
-                const uint4 v = *reinterpret_cast<const uint4*>(src + c * CD + half * LD);
+            for (int i = 0; i < 16; ++i) v[i] = acc[b][i];
 #pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    if constexpr (F32) {
-                        const float f[4] = {__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)};
+            for (int d = 16, m = 16; m > 1; d /= 2, m /= 2) {
+                const bool up = (lane & d) != 0;
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) s[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[b][c][x], f[x], s[b], 0, 0, 0);
-                    } else {
-                        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[b][c], __builtin_bit_cast(bf16x8_t, v), s[b], 0, 0, 0);
-                    }
+                for (int i = 0; i < m / 2; ++i) {
+                    const float give = up ? v[i] : v[i + m / 2], keep = up ? v[i + m / 2] : v[i];
+                    v[i] = keep + __shfl_xor(give, d);
                 }
             }
-            const int p = p0 + tok;
-            const bool counts = there && lse != -__builtin_inff();
-            const int see_hi = !counts ? 0 : a.causal ? p + 1 : 0x7fffffff, see_lo = a.window > 0 ? p - a.window + 1 : 0;
-            const bool masked = __any(see_hi < j0 + TOK || see_lo > j0);
-            const float lse2 = lse * kLog2e;
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], a.scale2, -lse2));
-                    if (masked) {
-                        const int j = j0 + b * 32 + (i / 4) * 8 + 4 * half + i % 4;
-                        w = j < see_hi && j >= see_lo ? w : 0.0f;
-                    }
-                    acc[b][i] += w;
-                }
-        }
-        // over the columns, then the waves
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float v = acc[b][i];
-#pragma unroll
-                for (int d = 1; d < 32; d *= 2) v += __shfl_xor(v, d);
-                if (n == 0) sh.w[wave][b * 32 + (i / 4) * 8 + 4 * half + i % 4] = v;
-            }
-        __syncthreads();
-        if (threadIdx.x < TOK) {
-            const int j = j0 + threadIdx.x;
-            const int64_t at = place(j);
-            if (at >= 0) {
-                const int t = threadIdx.x;
-                float w = (sh.w[0][t] + sh.w[1][t]) + (sh.w[2][t] + sh.w[3][t]);
-                if (j < p0 && a.decay != 0.0f) w += a.decay * a.scores[at];
-                a.scores[at] = w;
-            }
+            v[0] += __shfl_xor(v[0], 1);
+            const int i = (lane >> 1) & 15;      // (bits 16, 8, 4 and 2 of the lane, of the sum's number 8, 4, 2 and 1)
+            if ((lane & 1) == 0) sums[wave * WTOK + b * 32 + (i / 4) * 8 + 4 * half + i % 4] = v[0];
         }
         __syncthreads();
+        const int j = start + tid;
+        float w = tid < TOK ? sums[tid] : 0.0f;
+        if (pieces > 1) {
+            const int own = piece == 0 ? 2 * slot + 1 : 2 * (slot + piece);
+            if (tid < TOK) store_shared(a.part + (int64_t)own * TOK + tid, w);
+            if (!last_to_arrive(a.tickets + slot, (uint32_t)pieces, flag)) return;
+            if (tid < TOK) {
+                w = load_shared(a.part + (int64_t)(2 * slot + 1) * TOK + tid);
+#pragma unroll 4
+                for (int p = 1; p < pieces; ++p) w += load_shared(a.part + (int64_t)(2 * (slot + p)) * TOK + tid);
+            }
+        }
+        if (tid < TOK) {
+            const int64_t at = place_of(a, q, seq, h, j);
+            if (at >= 0) store_score(a, q, at, j, w);
+        }
     }
 };
 
-// Blocks take items (a sequence's tokens by TOK, and a head) in turn; 256 sequences at a time have theirs counted.
-template <typename T, bool FP8, int DP> __global__ __launch_bounds__(256, 1) void weights_kernel(WeightArgs a)
+struct WeightPlan {
+    int64_t few[kSeqs], many[kSeqs];   // units and steps of the sequences up to and with each
+    int64_t sums[2][4];
+};
+
+__device__ __forceinline__ int64_t scan64(int64_t v)
 {
-    typedef Weights<T, FP8, DP> W;
-    __shared__ Shared sh;
-    const int lane = lane_id(), wave = threadIdx.x >> 6;
-    int64_t before = 0;                                  // items of earlier chunks
-    for (int s0 = 0; s0 < a.c.S; s0 += 256) {
+    for (int d = 1; d < 64; d *= 2) {
+        const int64_t o = __shfl_up(v, d);
+        if (lane_id() >= d) v += o;
+    }
+    return v;
+}
+// The first sequence whose sum is above x.
+__device__ __forceinline__ int found_in(const int64_t* sums, int64_t x)
+{
+    int lo = 0, hi = kSeqs - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (sums[mid] > x) hi = mid;
+        else lo = mid + 1;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// LIGHT: all sequences are taken for ones of few rows.
+template <typename T, bool FP8, int DP, bool LIGHT> struct WeightKernel {
+    typedef FewWeights<T, FP8, DP> Few;
+    typedef ManyWeights<T, FP8, DP> Many;
+    static constexpr int BLOCKS = LIGHT ? (DP > 128 ? (sizeof(T) == 4 ? 1 : 2) : DP > 64 ? (sizeof(T) == 4 ? 2 : 3) : sizeof(T) == 4 ? 3 : 4) : (DP > 128 || sizeof(T) == 4 ? 1 : 2);      // of a unit
+    static constexpr size_t PLAN_AT = LIGHT ? 0 : (Many::LDS + 15) / 16 * 16, LDS = PLAN_AT + sizeof(WeightPlan);
+};
+template <typename T, bool FP8, int DP, bool LIGHT>
+__global__ __launch_bounds__(256, (WeightKernel<T, FP8, DP, LIGHT>::BLOCKS)) void weights_kernel(WeightArgs a)
+{
+    typedef WeightKernel<T, FP8, DP, LIGHT> K;
+    typedef typename K::Few Few;
+    typedef typename K::Many Many;
+    extern __shared__ __attribute__((aligned(256))) char smem[];
+    WeightPlan& plan = *reinterpret_cast<WeightPlan*>(smem + K::PLAN_AT);
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int Hk = a.c.Hk;
+    for (int s0 = 0; s0 < a.c.S; s0 += kSeqs) {
         const int s = s0 + threadIdx.x;
-        int count = 0;
+        int64_t few = 0, many = 0;
         if (s < a.c.S) {
-            const typename W::Seq q = W::seq_of(a, s);
-            count = q.held > q.lo ? (q.held - q.lo + W::TOK - 1) / W::TOK * a.c.Hk : 0;
-        }
-        int incl = wave_scan(count);
-        if (lane == 63) sh.sums[wave] = incl;
-        __syncthreads();
-        for (int w = 0; w < wave; ++w) incl += sh.sums[w];
-        sh.first[threadIdx.x] = incl;
-        __syncthreads();
-        const int total = sh.first[255];
-        const int64_t behind = before % gridDim.x;
-        for (int64_t i = (int64_t)blockIdx.x - behind + (blockIdx.x < behind ? gridDim.x : 0); i < total; i += gridDim.x) {
-            int lo = 0, hi = 255;                        // the first sequence whose items reach past i
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                if (sh.first[mid] > i) hi = mid;
-                else lo = mid + 1;
+            const WeightSeq q = seq_of(a, s);
+            if (LIGHT || q.n * a.G <= kFewRows) {
+                few = (int64_t)Few::units(q) * Hk;
+            } else if constexpr (!LIGHT) {
+                const Steps st = Many::steps_of(a, q);
+                many = Many::before(st, st.end) * Hk;
             }
-            lo = __builtin_amdgcn_readfirstlane(lo);
-            const int rem = (int)i - (lo > 0 ? sh.first[lo - 1] : 0);
-            const typename W::Seq q = W::seq_of(a, s0 + lo);
-            const int tile = a.c.Hk == 1 ? rem : (int)divided((uint32_t)rem, (uint32_t)a.c.Hk, a.hk_magic);
-            W::item(a, q, s0 + lo, rem - tile * a.c.Hk, q.lo + tile * W::TOK, sh);
         }
-        before += total;
+        few = scan64(few);
+        many = scan64(many);
+        if (lane == 63) {
+            plan.sums[0][wave] = few;
+            plan.sums[1][wave] = many;
+        }
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) {
+            few += plan.sums[0][w];
+            many += plan.sums[1][w];
+        }
+        plan.few[threadIdx.x] = few;
+        plan.many[threadIdx.x] = many;
+        __syncthreads();
+        if constexpr (!LIGHT) {
+            const int chunk = s0 / kSeqs;
+            const bool split = chunk < a.split_chunks;                       // (where there are no more slots, a tile is its first step's owner's)
+            const int64_t all = plan.many[kSeqs - 1];
+            const int64_t most = (all + kMinSteps - 1) / kMinSteps;
+            const int64_t blocks = most < gridDim.x ? most : gridDim.x;      // that have a stretch
+            auto cut = [&](int64_t b) { return b * all / blocks; };
+            if ((int64_t)blockIdx.x < blocks) {
+                // the stretch that step x lies in
+                auto owner = [&](int64_t x) {
+                    int64_t b = x * blocks / all;
+                    while (cut(b + 1) <= x) ++b;
+                    return (int)b;
+                };
+                int64_t x = cut(blockIdx.x);
+                const int64_t end = cut(blockIdx.x + 1);
+                while (x < end) {
+                    const int i = found_in(plan.many, x);
+                    const int64_t base = i > 0 ? plan.many[i - 1] : 0;
+                    const WeightSeq q = seq_of(a, s0 + i);
+                    const Steps st = Many::steps_of(a, q);
+                    const int64_t of_head = Many::before(st, st.end);
+                    const int h = (int)((x - base) / of_head);
+                    const int64_t head_base = base + h * of_head, rem = x - head_base;
+                    int lo = st.first, hi = st.end - 1;                      // the last tile that starts at or before rem
+                    while (lo < hi) {
+                        const int mid = (lo + hi + 1) / 2;
+                        if (Many::before(st, mid) <= rem) lo = mid;
+                        else hi = mid - 1;
+                    }
+                    const int64_t t_begin = head_base + Many::before(st, lo), t_end = head_base + Many::before(st, lo + 1);
+                    const int64_t to = !split || t_end < end ? t_end : end;
+                    if (split || x == t_begin) {
+                        const int first = split ? owner(t_begin) : (int)blockIdx.x, last = split ? owner(t_end - 1) : first;
+                        Many::run(a, q, st, s0 + i, h, lo, (int)(x - t_begin), (int)(to - t_begin), (int)blockIdx.x - first, last - first + 1,
+                                  chunk * (int)gridDim.x + first, smem);
+                    }
+                    x = to;
+                    __syncthreads();
+                }
+            }
+        }
+        const int64_t all = plan.few[kSeqs - 1], waves = (int64_t)gridDim.x * 4, me = (int64_t)blockIdx.x * 4 + wave;
+        int64_t x = me * all / waves;
+        const int64_t end = (me + 1) * all / waves;
+        while (x < end) {
+            const int i = found_in(plan.few, x);
+            const int64_t base = i > 0 ? plan.few[i - 1] : 0;
+            const WeightSeq q = seq_of(a, s0 + i);
+            const int units = Few::units(q), h = (int)((x - base) / units), from = (int)(x - base - (int64_t)h * units);
+            const int to = end - x < units - from ? from + (int)(end - x) : units;
+            const int start = q.lo & ~(Few::TOK - 1);
+            const int stop = start + to * Few::TOK < q.held ? start + to * Few::TOK : q.held;
+            Few::run(a, q, s0 + i, h, start + from * Few::TOK, stop);
+            x += to - from;
+        }
         __syncthreads();
     }
 }
 
-template <typename T, bool FP8, int DP> hipError_t launch(WeightArgs a, hipStream_t s)
+template <typename T, bool FP8, int DP, bool LIGHT> hipError_t launch(WeightArgs a, bool clear_tickets, hipStream_t s)
 {
-    // (the items of a chunk's sequences are counted in 32 bits)
-    const int64_t tiles = ((int64_t)a.c.max_pages << a.c.page_shift) / Weights<T, FP8, DP>::TOK + 1;
-    if (tiles * a.c.Hk > 0x7fffffff / (a.c.S < 256 ? a.c.S : 256)) return hipErrorInvalidConfiguration;
+    typedef WeightKernel<T, FP8, DP, LIGHT> K;
     int units = 0;
-    const hipError_t e = compute_units(&units);
+    hipError_t e = compute_units(&units);
     if (e != hipSuccess) return e;
     a.g_magic = a.G > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G) : 0;
-    a.hk_magic = a.c.Hk > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.c.Hk - 1) / a.c.Hk) : 0;
-    weights_kernel<T, FP8, DP><<<(unsigned)units * 2, 256, 0, s>>>(a);
+    static bool done[kMaxDevices];
+    const auto kern = weights_kernel<T, FP8, DP, LIGHT>;
+    e = ensure_lds_limit(kern, K::LDS, done);
+    if (e != hipSuccess) return e;
+    if (clear_tickets && (e = launch_fill_zero(a.tickets, kPartUnits, s)) != hipSuccess) return e;
+    int grid = units * K::BLOCKS;
+    if (grid > kPartUnits) grid = kPartUnits;      // (a ticket to a stretch)
+    a.split_chunks = (int)((int64_t)kPartUnits * 16 * a.c.D / (2 * K::Many::TOK) / grid);      // two slots of partial sums to a stretch
+    if (a.split_chunks > kPartUnits / grid) a.split_chunks = kPartUnits / grid;
+    kern<<<(unsigned)grid, 256, K::LDS, s>>>(a);
     return hipGetLastError();
 }
 
-template <typename T, bool FP8> hipError_t launch_by_dim(const WeightArgs& a, hipStream_t s)
+template <typename T, bool FP8, int DP> hipError_t launch_by_rows(const WeightArgs& a, bool clear, hipStream_t s)
 {
-    if (a.c.D <= 64) return launch<T, FP8, 64>(a, s);
-    if (a.c.D <= 128) return launch<T, FP8, 128>(a, s);
-    return launch<T, FP8, 256>(a, s);
+    // (the rule of the attention's launch: batches of decode or drafted rows alone)
+    constexpr int kMostRows = 384;
+    const int64_t rows = a.c.T, seqs = a.c.S, most = rows < seqs ? rows : rows - seqs + 1;
+    const bool light = rows * a.G <= kFewRows * seqs && most * a.G <= kMostRows;
+    return light ? launch<T, FP8, DP, true>(a, clear, s) : launch<T, FP8, DP, false>(a, clear, s);
+}
+
+template <typename T, bool FP8> hipError_t launch_by_dim(const WeightArgs& a, bool clear, hipStream_t s)
+{
+    if (a.c.D <= 64) return launch_by_rows<T, FP8, 64>(a, clear, s);
+    if (a.c.D <= 128) return launch_by_rows<T, FP8, 128>(a, clear, s);
+    return launch_by_rows<T, FP8, 256>(a, clear, s);
 }
 
 }  // namespace
 
-hipError_t launch_kv_weights(int dtype, bool fp8, const WeightArgs& a, hipStream_t s)
+hipError_t launch_kv_weights(int dtype, bool fp8, const WeightArgs& a, bool clear, hipStream_t s)
 {
-    if (dtype == MOE_BF16) return fp8 ? launch_by_dim<bf16_t, true>(a, s) : launch_by_dim<bf16_t, false>(a, s);
-    return fp8 ? launch_by_dim<float, true>(a, s) : launch_by_dim<float, false>(a, s);
+    if (dtype == MOE_BF16) return fp8 ? launch_by_dim<bf16_t, true>(a, clear, s) : launch_by_dim<bf16_t, false>(a, clear, s);
+    return fp8 ? launch_by_dim<float, true>(a, clear, s) : launch_by_dim<float, false>(a, clear, s);
 }
 
 }  // namespace moe

@@ -73,9 +73,6 @@ def test_weights():
         assert c.keep_status("weights", decay=decay) == SHAPE
     assert c.keep_status("weights", lse=None) == NULL and c.keep_status("weights", lse=FAKE + 2) == ALIGN
     assert c.keep_status("weights", scores=None) == NULL and c.keep_status("weights", scores=FAKE + 8) == ALIGN
-    # more tokens and heads than are counted
-    wide = Call(heads=4096, kv_heads=4096, dim=16)
-    assert wide.keep_status("weights", T=1, batch={"n_seqs": 300, "max_pages": 2 ** 17}) == SHAPE
 
 
 @pytest.mark.parametrize("what", ["select", "compact"])
