@@ -267,6 +267,7 @@ moe_status moe_kv_weights(moe_kv_ctx* ctx, const void* q, int64_t ldq, const flo
     if ((opt->causal != 0 && opt->causal != 1) || opt->window < 0 || opt->window > 1 << 30 || !(opt->decay >= 0.0f && opt->decay <= 1.0f))
         return MOE_ERR_SHAPE;
     if (T == 0) return MOE_OK;
+    if (ldq > 1 << 23) return MOE_ERR_SHAPE;      // (rows of a step lie within 2^31 bytes)
     if (!lse || !scores) return MOE_ERR_NULL;
     const moe_kv_config& g = ctx->cfg;
     if ((st = check_rows(g, q, ldq, (int64_t)g.heads * g.dim)) != MOE_OK) return st;

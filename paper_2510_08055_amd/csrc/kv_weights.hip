@@ -5,16 +5,17 @@
 // stream by (read once: that bounds it); for many rows the keys of 64 tokens stay in a wave's registers and the rows pass by.
 //
 // Work is cut on the device, from the descriptors, into equal stretches: of 32-token units of all sequences and heads, a stretch to a wave, where rows are
-// few; where they are many, of steps (64 packed rows by 256 tokens), a stretch to a block.  A token's sum belongs to one wave, or is joined from the
+// few; where they are many, of steps (128 packed rows by 256 tokens), a stretch to a block.  A token's sum belongs to one wave, or is joined from the
 // stretches that its tokens' steps fall into, in their order, by the block that ends the last: there are no atomic sums, and a batch's result is always the same bits.
-#include "attention_plan.h"
+#include "attention_tile.h"
 
 namespace moe {
 namespace {
 
 constexpr int kSeqs = 256;             // sequences that are planned at a time, a thread each
 constexpr int kFewRows = 16;           // packed rows of a sequence up to which they stay in registers
-constexpr int kMinSteps = 8;           // of a stretch, where there are too few for all blocks
+constexpr int kRounds = 2;              // stretches of many rows to a place on a unit: the steps at a causal border take less time
+constexpr int kMinSteps = 4;           // of a stretch, where there are too few for all blocks
 
 __device__ __forceinline__ int token_of(const WeightArgs& a, int r) { return a.G == 1 ? r : (int)divided((uint32_t)r, (uint32_t)a.G, a.g_magic); }
 
@@ -44,11 +45,7 @@ __device__ __forceinline__ int64_t place_of(const WeightArgs& a, const WeightSeq
 }
 
 // A row's lse as a power of two; infinity where the row adds nothing.
-__device__ __forceinline__ float lse2_of(const WeightArgs& a, int64_t row, int head)
-{
-    const float v = a.lse[row * a.Hq + head];
-    return v == -__builtin_inff() ? __builtin_inff() : v * kLog2e;
-}
+__device__ __forceinline__ float lse2_of(float lse) { return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e; }
 
 __device__ __forceinline__ void store_score(const WeightArgs& a, const WeightSeq& q, int64_t at, int j, float w)
 {
@@ -56,10 +53,32 @@ __device__ __forceinline__ void store_score(const WeightArgs& a, const WeightSeq
     a.scores[at] = w;
 }
 
+// A value that what follows from it is not computed ahead of: the loops over stretches would keep all of that in registers.
+__device__ __forceinline__ int here(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// The sum over the lane's row of sixteen.
+__device__ __forceinline__ float over_sixteen(float v)
+{
+    auto turn = [&](auto ctrl) {
+        v += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), decltype(ctrl)::value, 0xF, 0xF, true));
+    };
+    using std::integral_constant;
+    turn(integral_constant<int, 0x128>{});      // from 8, 4, 2 and 1 lanes around the sixteen
+    turn(integral_constant<int, 0x124>{});
+    turn(integral_constant<int, 0x122>{});
+    turn(integral_constant<int, 0x121>{});
+    return v;
+}
+
 // ---- few rows ----
-template <typename T, bool FP8, int DP> struct FewWeights {
+// NJ: 16-token subtiles of a step, as the registers allow.
+template <typename T, bool FP8, int DP, int NJ> struct FewWeights {
     static constexpr bool F32 = sizeof(T) == 4;
-    static constexpr int NJ = F32 ? 1 : 2, TOK = NJ * 16;          // 16-token subtiles of a step
+    static constexpr int TOK = NJ * 16;
     static constexpr int ESZ = FP8 ? 1 : (int)sizeof(T);
     static constexpr int KC = DP / (F32 ? 16 : (FP8 ? 64 : 32));   // key loads per subtile
     static constexpr int KDIM = F32 ? 4 : (FP8 ? 16 : 8);          // dimensions of such a load
@@ -81,7 +100,7 @@ template <typename T, bool FP8, int DP> struct FewWeights {
         const int tok = there ? token_of(a, r) : 0, head = h * a.G + (there ? r - tok * a.G : 0);
         const int64_t row = q.row0 + tok;
         const T* src = static_cast<const T*>(a.q) + row * a.ldq + (int64_t)head * D;
-        Q.lse2 = lse2_of(a, row, head);
+        Q.lse2 = lse2_of(a.lse[row * a.Hq + head]);
         const int p = q.p0 + tok;
         Q.see_hi = !there || Q.lse2 == __builtin_inff() ? 0 : a.causal ? p + 1 : 0x7fffffff;
         Q.see_lo = a.window > 0 ? p - a.window + 1 : 0;
@@ -108,7 +127,7 @@ template <typename T, bool FP8, int DP> struct FewWeights {
     // Tokens [begin, end) of a sequence and head, begin a multiple of TOK; a wave's.
     static __device__ __forceinline__ void run(const WeightArgs& a, const WeightSeq& q, int seq, int h, int begin, int end)
     {
-        const int lane = lane_id(), n = lane & 15, g = lane >> 4, D = a.c.D, shift = a.c.page_shift;
+        const int lane = here(lane_id()), n = lane & 15, g = lane >> 4, D = a.c.D, shift = a.c.page_shift;
         Entries pages;
         pages.hold(a.c, seq, begin >> shift, end);
         const int rows = q.n * a.G;
@@ -153,6 +172,7 @@ template <typename T, bool FP8, int DP> struct FewWeights {
             // the keys as the first product's operand
             bf16x8_t kb[F32 ? 1 : NJ][F32 ? 1 : DP / 32];
             float kf[F32 ? DP / 16 : 1][4];
+            static_assert(!F32 || NJ == 1, "one subtile's keys");
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
                 float sc = 1.0f;
@@ -215,15 +235,7 @@ template <typename T, bool FP8, int DP> struct FewWeights {
             for (int j = 0; j < NJ; ++j)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    float v = sum[j][r];
-                    auto turn = [&](auto ctrl) {
-                        v += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), decltype(ctrl)::value, 0xF, 0xF, true));
-                    };
-                    using std::integral_constant;
-                    turn(integral_constant<int, 0x128>{});      // from 8, 4, 2 and 1 lanes around the sixteen
-                    turn(integral_constant<int, 0x124>{});
-                    turn(integral_constant<int, 0x122>{});
-                    turn(integral_constant<int, 0x121>{});
+                    const float v = over_sixteen(sum[j][r]);
                     w = n == j * 4 + r ? v : w;
                 }
             if (x.at >= 0) a.scores[x.at] = __builtin_fmaf(a.decay, x.old, w);
@@ -233,6 +245,12 @@ template <typename T, bool FP8, int DP> struct FewWeights {
 };
 
 // ---- many rows ----
+// A dword to a lane, straight into LDS, one after the other.
+__device__ __forceinline__ void load_lds_dword(uint32_t off, const char* base, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory");
+}
+
 // The steps of a sequence and head: tiles of TOK tokens, of each of which the rows that see it are taken ROWS at a time.  Tiles start at the
 // position of the first row, or a whole number of tiles from it, so that the rows a causal mask leaves out are whole steps.
 struct Steps {
@@ -242,15 +260,23 @@ struct Steps {
     int less;                          // by which each tile from t0 on has its rows start later (causal)
     int each;                          // steps of a tile, where they are the same for all; 0: all rows from the first that sees it
 };
-template <typename T, bool FP8, int DP> struct ManyWeights {
+// EXACT: the heads are DP wide, no less.
+template <typename T, bool FP8, int DP, bool EXACT> struct ManyWeights {
     static constexpr bool F32 = sizeof(T) == 4;
-    static constexpr int NB = F32 && DP > 128 ? 1 : 2, WTOK = 32 * NB, TOK = 4 * WTOK;      // tokens of a wave, of a block
-    static constexpr int ROWS = F32 ? 32 : 64;
+    static constexpr int WAVES = 8, WTOK = 32, TOK = WAVES * WTOK;         // tokens of a wave, of a block
+    static constexpr int ROWS = F32 ? 64 : 128, PARTS = ROWS / 32;         // rows of a stage
     static constexpr int CD = F32 ? 8 : 16, KC = DP / CD, LD = CD / 2;      // dimensions of a step of the product, steps, dimensions of a lane in it
     static constexpr int ROWB = DP * (int)sizeof(T), CH = ROWB / 16;        // bytes of a row in LDS, its 16-byte chunks
-    static constexpr int LOADS = ROWS * CH / 256;
     static constexpr int STAGE = ROWS * ROWB;
-    static constexpr size_t LDS = 2 * STAGE + 2 * ROWS * 4 + TOK * 4 + 16;  // rows, their lse, a tile's sums, a flag
+    static constexpr int LOADS = STAGE / (WAVES * 1024), AT = 64 / CH;                // of a wave for a stage, 1 KB each, and the rows of one
+    static constexpr size_t LDS = 2 * (STAGE + ROWS * 4) + TOK * 4 + 16;    // rows and their lse, a tile's sums, a flag
+
+    // Place of chunk 0 of row r: distinct for the rows that one read touches.
+    static __device__ __forceinline__ int swz(int r)
+    {
+        if constexpr (ROWB == 128) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+        else return ((r & 3) << 2) | ((r >> 2) & 3);
+    }
 
     static __device__ __forceinline__ Steps steps_of(const WeightArgs& a, const WeightSeq& q)
     {
@@ -275,66 +301,51 @@ template <typename T, bool FP8, int DP> struct ManyWeights {
         return (whole > 0 ? whole * s.total : 0) + m * s.total - s.less * (m * (m - 1) / 2 + m * skip);
     }
 
-    static __device__ __forceinline__ int swz(int r)
-    {
-        if constexpr (ROWB == 128) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
-        else return ((r & 3) << 2) | ((r >> 2) & 3);
-    }
-
+    typedef __attribute__((address_space(3))) uint32x4_t lds_chunk_t;
     struct Keys {
-        bf16x8_t b[F32 ? 1 : NB][F32 ? 1 : KC];
-        float f[F32 ? NB : 1][F32 ? KC : 1][4];
+        bf16x8_t b[F32 ? 1 : KC];
+        float f[F32 ? KC : 1][4];
     };
-    static __device__ __forceinline__ void load_keys(const WeightArgs& a, const WeightSeq& q, int seq, int h, int j0, Keys& K)
+    static __device__ __forceinline__ void load_keys(const WeightArgs& a, int64_t row, int half, Keys& K)
     {
-        const int lane = lane_id(), n = lane & 31, half = lane >> 5, D = a.c.D;
-        int64_t row[NB];
+        const int D = EXACT ? DP : a.c.D;
+        float sc = 1.0f;
+        if constexpr (FP8) sc = scale_of(a.c.ks[row]);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) row[b] = place_of(a, q, seq, h, j0 + b * 32 + n);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            if (row[b] < 0) row[b] = 0;          // (a token that is not there: some row, its sum is not stored)
-            float sc = 1.0f;
-            if constexpr (FP8) sc = scale_of(a.c.ks[row[b]]);
-#pragma unroll
-            for (int c = 0; c < KC; ++c) {
-                const int d = c * CD + half * LD;
-                const bool in = d < D;           // (past the dimension: zeros, like the rows)
-                const char* p = a.c.k + (row[b] * D + (in ? d : 0)) * (FP8 ? 1 : (int)sizeof(T));
-                if constexpr (F32) {
-                    float4 v;
-                    if constexpr (FP8) {
-                        const int u = *reinterpret_cast<const int*>(p);
-                        const hw_float2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8(u, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(u, true);
-                        v = make_float4(lo[0] * sc, lo[1] * sc, hi[0] * sc, hi[1] * sc);
-                    } else {
-                        v = *reinterpret_cast<const float4*>(p);
-                    }
-                    K.f[b][c][0] = in ? v.x : 0; K.f[b][c][1] = in ? v.y : 0; K.f[b][c][2] = in ? v.z : 0; K.f[b][c][3] = in ? v.w : 0;
-                } else if constexpr (FP8) {
-                    const uint2 u = *reinterpret_cast<const uint2*>(p);
-                    const uint32_t w[2] = {in ? u.x : 0, in ? u.y : 0};
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const bf16x2_t lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], sc, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], sc, true);
-                        K.b[b][c][4 * i] = lo[0]; K.b[b][c][4 * i + 1] = lo[1]; K.b[b][c][4 * i + 2] = hi[0]; K.b[b][c][4 * i + 3] = hi[1];
-                    }
+        for (int c = 0; c < KC; ++c) {
+            const int d = c * CD + half * LD;
+            const char* p = a.c.k + (row * D + (d < D ? d : 0)) * (FP8 ? 1 : (int)sizeof(T));
+            if constexpr (F32) {
+                float4 v;
+                if constexpr (FP8) {
+                    const int u = *reinterpret_cast<const int*>(p);
+                    const hw_float2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8(u, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(u, true);
+                    v = make_float4(lo[0] * sc, lo[1] * sc, hi[0] * sc, hi[1] * sc);
                 } else {
-                    uint4 v = *reinterpret_cast<const uint4*>(p);
-                    if (!in) v = make_uint4(0, 0, 0, 0);
-                    K.b[b][c] = __builtin_bit_cast(bf16x8_t, v);
+                    v = *reinterpret_cast<const float4*>(p);
                 }
+                K.f[c][0] = v.x; K.f[c][1] = v.y; K.f[c][2] = v.z; K.f[c][3] = v.w;
+            } else if constexpr (FP8) {
+                const uint2 u = *reinterpret_cast<const uint2*>(p);
+                const uint32_t w[2] = {u.x, u.y};
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const bf16x2_t lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], sc, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], sc, true);
+                    K.b[c][4 * i] = lo[0]; K.b[c][4 * i + 1] = lo[1]; K.b[c][4 * i + 2] = hi[0]; K.b[c][4 * i + 3] = hi[1];
+                }
+            } else {
+                K.b[c] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(p));
             }
         }
     }
 
-    // Steps [x0, x1) of a tile's `count`, as piece `piece` of `pieces`; slot: where piece 0 leaves its sums, and its ticket.
+    // Steps [x0, x1) of a tile's `count`, as piece `piece` of `pieces`; ticket: of the tile, and where piece 0 leaves its sums.
     static __device__ __forceinline__ void run(const WeightArgs& a, const WeightSeq& q, const Steps& st, int seq, int h, int tile, int x0, int x1, int piece,
-                                               int pieces, int slot, char* smem)
+                                               int pieces, int ticket, char* smem)
     {
-        const int tid = threadIdx.x, lane = lane_id(), n = lane & 31, half = lane >> 5;
+        const int tid = here(threadIdx.x), lane = tid & 63, n = lane & 31, half = lane >> 5;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const int D = a.c.D, rows = q.n * a.G;
+        const int D = EXACT ? DP : a.c.D, rows = q.n * a.G;
         float* const lse = reinterpret_cast<float*>(smem + 2 * STAGE);
         float* const sums = lse + 2 * ROWS;
         int32_t* const flag = reinterpret_cast<int32_t*>(sums + TOK);
@@ -344,137 +355,126 @@ template <typename T, bool FP8, int DP> struct ManyWeights {
         int r0 = (int64_t)(skip + x0) * ROWS < rows ? (skip + x0) * ROWS : rows;
         const int r1 = (int64_t)(skip + x1) * ROWS < rows ? (skip + x1) * ROWS : rows;
 
-        Keys K;
-        load_keys(a, q, seq, h, j0, K);
-
-        // a stage's rows: 16 bytes to a thread and load
-        uint4 raw[LOADS];
-        float raw_lse = 0;
-        auto row_at = [&](int r, int64_t& row, int& head) {
+        // A stage's rows go straight into LDS, chunk c of row r to place c ^ swz(r).  A load has AT of them: where they are of one token, or of whole
+        // tokens, only its address goes on from load to load; else, and where there are no more rows (the last one stands for them), every lane finds its own.
+        // (Rows of a load lie within 2^31 bytes: the launch sees to it.)
+        const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_address(smem));
+        const int stride = (int)a.ldq * (int)sizeof(T), rowb = D * (int)sizeof(T);
+        const bool even = a.G % AT == 0 || AT % a.G == 0;
+        constexpr int PER = ROWS / WAVES;        // rows of a wave's lse
+        auto aim = [&](int r, int tok0, int chunk) {
             const int rr = r < rows ? r : rows - 1, tok = token_of(a, rr);
-            row = q.row0 + tok;
-            head = h * a.G + rr - tok * a.G;
+            // (chunks past the dimension: no product reads them)
+            return (uint32_t)((tok - tok0) * stride + (rr - tok * a.G) * rowb + (chunk * 16 < rowb ? chunk * 16 : 0));
         };
-        auto fetch = [&](int from) {
+        const uint32_t lane_off = (uint32_t)(a.G % AT == 0 ? lane / CH * rowb : lane / CH / a.G * stride + lane / CH % a.G * rowb);
+        auto fetch = [&](int first, int slot) {
+            const bool all = even && first + ROWS <= rows;
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
-                const int at = i * 256 + tid, chunk = at % CH;
-                int64_t row;
-                int head;
-                row_at(from + at / CH, row, head);
-                const char* src = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + row * a.ldq + (int64_t)head * D);
-                const bool in = chunk * 16 < D * (int)sizeof(T);
-                raw[i] = *reinterpret_cast<const uint4*>(src + (in ? chunk * 16 : 0));
-                if (!in) raw[i] = make_uint4(0, 0, 0, 0);
+                const int lr = (wave * LOADS + i) * AT, r = first + lr;
+                const int rr = r < rows ? r : rows - 1, tok = token_of(a, rr);
+                const int chunk = (lane % CH) ^ swz(lr + lane / CH);
+                const char* base = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (int64_t)(q.row0 + tok) * a.ldq + (int64_t)h * a.G * D);
+                const uint32_t off[1] = {all ? lane_off + (chunk * 16 < rowb ? chunk * 16 : 0) : aim(r + lane / CH, tok, chunk)};
+                load_lds_group(off, all ? base + (r - tok * a.G) * rowb : base, lds0 + slot * STAGE + lr * ROWB);
             }
-            if (tid < ROWS) {
-                int64_t row;
-                int head;
-                row_at(from + tid, row, head);
-                raw_lse = from + tid < rows ? lse2_of(a, row, head) : __builtin_inff();
+            if (lane < PER) {
+                const int r = first + wave * PER + lane, rr = r < rows ? r : rows - 1, tok = token_of(a, rr), tok0 = token_of(a, first);
+                load_lds_dword((uint32_t)((tok - tok0) * a.Hq + rr - tok * a.G) * 4, reinterpret_cast<const char*>(a.lse + (int64_t)(q.row0 + tok0) * a.Hq + h * a.G),
+                               lds0 + 2 * STAGE + (slot * ROWS + wave * PER) * 4);
             }
         };
-        auto put = [&](int stage) {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int at = i * 256 + tid, r = at / CH, chunk = at % CH;
-                *reinterpret_cast<uint4*>(smem + stage * STAGE + r * ROWB + ((chunk ^ swz(r)) * 16)) = raw[i];
-            }
-            if (tid < ROWS) lse[stage * ROWS + tid] = raw_lse;
-        };
-
-        float acc[NB][16];
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[b][i] = 0;
-        if (r0 < r1) {
-            fetch(r0);
-            put(0);
+        if (r0 < r1) fetch(r0, 0);
+        Keys K;
+        {
+            const int64_t row = place_of(a, q, seq, h, j0 + n);
+            load_keys(a, row < 0 ? 0 : row, half, K);      // (a token that is not there: some row, its sum is not stored)
         }
-        int stage = 0;
-        for (; r0 < r1; r0 += ROWS, stage ^= 1) {
-            __syncthreads();
-            const bool more = r0 + ROWS < r1;
-            if (more) fetch(r0 + ROWS);
+        float acc[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[i] = 0;
+
+        // 32 rows of a stage with the wave's tokens
+        auto product = [&](int slot, int part) {
+            const uint32_t at = lds0 + slot * STAGE + (part * 32 + n) * ROWB + ((half ^ swz(n)) * 16);
+            float16_t x = float16_t{};
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+                if (!EXACT && c * CD >= D) break;
+                const uint4 v = __builtin_bit_cast(uint4, *(const lds_chunk_t*)(uintptr_t)(at ^ (uint32_t)(c * 32)));
+                if constexpr (F32) {
+                    const float f[4] = {__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_mfma_f32_32x32x2f32(K.f[c][i], f[i], x, 0, 0, 0);
+                } else {
+                    x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(K.b[c], __builtin_bit_cast(bf16x8_t, v), x, 0, 0, 0);
+                }
+            }
+            return x;
+        };
+        int slot = 0;
+        for (; r0 < r1; r0 += ROWS, slot ^= 1) {
+            wait_vmcnt<0>();
+            block_barrier();
+            if (r0 + ROWS < r1) fetch(r0 + ROWS, slot ^ 1);
+            if (j0 >= q.held) continue;
+            const float* const l = lse + slot * ROWS;
+            const int p_first = q.p0 + token_of(a, r0), r_last = r0 + ROWS <= rows ? r0 + ROWS - 1 : rows - 1, p_last = q.p0 + token_of(a, r_last);
+            if (a.causal && p_last < j0) continue;                             // (no row sees a token of the wave)
+            bool none = false;
+#pragma unroll
+            for (int i = 0; i < ROWS; i += 64) none |= l[i + lane] == -__builtin_inff();
+            if (r0 + ROWS <= rows && (!a.causal || p_first >= j1) && (a.window == 0 || p_last - a.window + 1 <= j0) && !__any(none)) {
+                // every row sees every token of the wave
 #pragma unroll 1
-            for (int part = 0; part < ROWS / 32; ++part) {
+                for (int part = 0; part < PARTS; ++part) {
+                    const float l2 = l[part * 32 + n] * kLog2e;
+                    const float16_t x = product(slot, part);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale2, -l2));
+                }
+                continue;
+            }
+#pragma unroll 1
+            for (int part = 0; part < PARTS; ++part) {
                 const int first = r0 + part * 32;
                 if (first >= rows) break;
                 const int last = first + 31 < rows ? first + 31 : rows - 1;
-                const int p_first = q.p0 + token_of(a, first), p_last = q.p0 + token_of(a, last);
-                if ((a.causal && p_last < j0) || (a.window > 0 && p_first - a.window + 1 > j1)) continue;      // none of the rows sees a token of the wave
-                const char* at = smem + stage * STAGE + (part * 32 + n) * ROWB;
-                const float l2 = lse[stage * ROWS + part * 32 + n];
-                float16_t s[NB];
+                if ((a.causal && q.p0 + token_of(a, last) < j0) || (a.window > 0 && q.p0 + token_of(a, first) - a.window + 1 > j1)) continue;
+                const int r = first + n, p = q.p0 + token_of(a, r < rows ? r : rows - 1);
+                const float raw = l[part * 32 + n], l2 = raw * kLog2e;
+                const int see_hi = raw == -__builtin_inff() || r >= rows ? start : a.causal ? p + 1 : 0x7fffffff, see_lo = a.window > 0 ? p - a.window + 1 : -0x7fffffff;
+                const float16_t x = product(slot, part);
 #pragma unroll
-                for (int b = 0; b < NB; ++b) s[b] = float16_t{};
-#pragma unroll
-                for (int c = 0; c < KC; ++c) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(at + (((2 * c + half) ^ swz(n)) * 16));
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) {
-                        if constexpr (F32) {
-                            const float f[4] = {__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)};
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) s[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(K.f[b][c][i], f[i], s[b], 0, 0, 0);
-                        } else {
-                            s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(K.b[b][c], __builtin_bit_cast(bf16x8_t, v), s[b], 0, 0, 0);
-                        }
-                    }
-                }
-                const bool masked = (a.causal && p_first < j1) || (a.window > 0 && p_last - a.window + 1 > j0) || __any(l2 == __builtin_inff());
-                if (!masked) {
-#pragma unroll
-                    for (int b = 0; b < NB; ++b)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[b][i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], a.scale2, -l2));
-                } else {
-                    const int p = q.p0 + token_of(a, first + n < rows ? first + n : rows - 1);
-                    const int see_hi = l2 == __builtin_inff() ? start : a.causal ? p + 1 : 0x7fffffff, see_lo = a.window > 0 ? p - a.window + 1 : -0x7fffffff;
-#pragma unroll
-                    for (int b = 0; b < NB; ++b)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int j = j0 + b * 32 + (i / 4) * 8 + 4 * half + i % 4;
-                            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], a.scale2, -l2));
-                            acc[b][i] += ((j < see_hi) & (j >= see_lo)) ? w : 0.0f;
-                        }
+                for (int i = 0; i < 16; ++i) {
+                    const int j = j0 + (i / 4) * 8 + 4 * half + i % 4;
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale2, -l2));
+                    acc[i] += ((j < see_hi) & (j >= see_lo)) ? w : 0.0f;
                 }
             }
-            if (more) put(stage ^ 1);
         }
 
-        // over the 32 columns: halves of the sums change sides with half of the lanes, until a lane has one
+        // over the 32 columns; lane n keeps the sum of the token whose number is n's
+        float mine = 0;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            float v[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = acc[b][i];
-#pragma unroll
-            for (int d = 16, m = 16; m > 1; d /= 2, m /= 2) {
-                const bool up = (lane & d) != 0;
-#pragma unroll
-                for (int i = 0; i < m / 2; ++i) {
-                    const float give = up ? v[i] : v[i + m / 2], keep = up ? v[i + m / 2] : v[i];
-                    v[i] = keep + __shfl_xor(give, d);
-                }
-            }
-            v[0] += __shfl_xor(v[0], 1);
-            const int i = (lane >> 1) & 15;      // (bits 16, 8, 4 and 2 of the lane, of the sum's number 8, 4, 2 and 1)
-            if ((lane & 1) == 0) sums[wave * WTOK + b * 32 + (i / 4) * 8 + 4 * half + i % 4] = v[0];
+        for (int i = 0; i < 16; ++i) {
+            const float v = over_sixteen(acc[i]);
+            mine = (n & 15) == i ? v : mine;
         }
+        const auto other = __builtin_amdgcn_permlane16_swap(__float_as_uint(mine), __float_as_uint(mine), false, false);
+        if (n < 16) sums[wave * WTOK + (n / 4) * 8 + 4 * half + n % 4] = __uint_as_float(other[0]) + __uint_as_float(other[1]);
         __syncthreads();
         const int j = start + tid;
         float w = tid < TOK ? sums[tid] : 0.0f;
         if (pieces > 1) {
-            const int own = piece == 0 ? 2 * slot + 1 : 2 * (slot + piece);
+            const int own = piece == 0 ? 2 * ticket + 1 : 2 * (ticket + piece);
             if (tid < TOK) store_shared(a.part + (int64_t)own * TOK + tid, w);
-            if (!last_to_arrive(a.tickets + slot, (uint32_t)pieces, flag)) return;
+            if (!last_to_arrive(a.tickets + ticket, (uint32_t)pieces, flag)) return;
             if (tid < TOK) {
-                w = load_shared(a.part + (int64_t)(2 * slot + 1) * TOK + tid);
+                w = load_shared(a.part + (int64_t)(2 * ticket + 1) * TOK + tid);
 #pragma unroll 4
-                for (int p = 1; p < pieces; ++p) w += load_shared(a.part + (int64_t)(2 * (slot + p)) * TOK + tid);
+                for (int p = 1; p < pieces; ++p) w += load_shared(a.part + (int64_t)(2 * (ticket + p)) * TOK + tid);
             }
         }
         if (tid < TOK) {
@@ -486,7 +486,7 @@ template <typename T, bool FP8, int DP> struct ManyWeights {
 
 struct WeightPlan {
     int64_t few[kSeqs], many[kSeqs];   // units and steps of the sequences up to and with each
-    int64_t sums[2][4];
+    int64_t sums[2][8];
 };
 
 __device__ __forceinline__ int64_t scan64(int64_t v)
@@ -510,16 +510,18 @@ __device__ __forceinline__ int found_in(const int64_t* sums, int64_t x)
 }
 
 // LIGHT: all sequences are taken for ones of few rows.
-template <typename T, bool FP8, int DP, bool LIGHT> struct WeightKernel {
-    typedef FewWeights<T, FP8, DP> Few;
-    typedef ManyWeights<T, FP8, DP> Many;
-    static constexpr int BLOCKS = LIGHT ? (DP > 128 ? (sizeof(T) == 4 ? 1 : 2) : DP > 64 ? (sizeof(T) == 4 ? 2 : 3) : sizeof(T) == 4 ? 3 : 4) : (DP > 128 || sizeof(T) == 4 ? 1 : 2);      // of a unit
+template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> struct WeightKernel {
+    static constexpr bool F32 = sizeof(T) == 4;
+    typedef FewWeights<T, FP8, DP, F32 || (!LIGHT && DP > 64) ? 1 : 2> Few;
+    typedef ManyWeights<T, FP8, DP, EXACT> Many;
+    static constexpr int THREADS = LIGHT ? 256 : 64 * Many::WAVES;
+    static constexpr int BLOCKS = LIGHT ? (DP > 128 ? (F32 ? 1 : 2) : DP > 64 ? (F32 ? 2 : 3) : F32 ? 3 : 4) : DP > 128 || (F32 && DP > 64) ? 1 : 2;      // of a unit
     static constexpr size_t PLAN_AT = LIGHT ? 0 : (Many::LDS + 15) / 16 * 16, LDS = PLAN_AT + sizeof(WeightPlan);
 };
-template <typename T, bool FP8, int DP, bool LIGHT>
-__global__ __launch_bounds__(256, (WeightKernel<T, FP8, DP, LIGHT>::BLOCKS)) void weights_kernel(WeightArgs a)
+template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT>
+__global__ __launch_bounds__((WeightKernel<T, FP8, DP, EXACT, LIGHT>::THREADS), (WeightKernel<T, FP8, DP, EXACT, LIGHT>::BLOCKS * WeightKernel<T, FP8, DP, EXACT, LIGHT>::THREADS / 256)) void weights_kernel(WeightArgs a)
 {
-    typedef WeightKernel<T, FP8, DP, LIGHT> K;
+    typedef WeightKernel<T, FP8, DP, EXACT, LIGHT> K;
     typedef typename K::Few Few;
     typedef typename K::Many Many;
     extern __shared__ __attribute__((aligned(256))) char smem[];
@@ -529,7 +531,7 @@ __global__ __launch_bounds__(256, (WeightKernel<T, FP8, DP, LIGHT>::BLOCKS)) voi
     for (int s0 = 0; s0 < a.c.S; s0 += kSeqs) {
         const int s = s0 + threadIdx.x;
         int64_t few = 0, many = 0;
-        if (s < a.c.S) {
+        if (threadIdx.x < kSeqs && s < a.c.S) {
             const WeightSeq q = seq_of(a, s);
             if (LIGHT || q.n * a.G <= kFewRows) {
                 few = (int64_t)Few::units(q) * Hk;
@@ -549,8 +551,10 @@ __global__ __launch_bounds__(256, (WeightKernel<T, FP8, DP, LIGHT>::BLOCKS)) voi
             few += plan.sums[0][w];
             many += plan.sums[1][w];
         }
-        plan.few[threadIdx.x] = few;
-        plan.many[threadIdx.x] = many;
+        if (threadIdx.x < kSeqs) {
+            plan.few[threadIdx.x] = few;
+            plan.many[threadIdx.x] = many;
+        }
         __syncthreads();
         if constexpr (!LIGHT) {
             const int chunk = s0 / kSeqs;
@@ -594,7 +598,7 @@ __global__ __launch_bounds__(256, (WeightKernel<T, FP8, DP, LIGHT>::BLOCKS)) voi
                 }
             }
         }
-        const int64_t all = plan.few[kSeqs - 1], waves = (int64_t)gridDim.x * 4, me = (int64_t)blockIdx.x * 4 + wave;
+        const int64_t all = plan.few[kSeqs - 1], waves = (int64_t)gridDim.x * (K::THREADS / 64), me = (int64_t)blockIdx.x * (K::THREADS / 64) + wave;
         int64_t x = me * all / waves;
         const int64_t end = (me + 1) * all / waves;
         while (x < end) {
@@ -612,23 +616,23 @@ __global__ __launch_bounds__(256, (WeightKernel<T, FP8, DP, LIGHT>::BLOCKS)) voi
     }
 }
 
-template <typename T, bool FP8, int DP, bool LIGHT> hipError_t launch(WeightArgs a, bool clear_tickets, hipStream_t s)
+template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> hipError_t launch(WeightArgs a, bool clear_tickets, hipStream_t s)
 {
-    typedef WeightKernel<T, FP8, DP, LIGHT> K;
+    typedef WeightKernel<T, FP8, DP, EXACT, LIGHT> K;
     int units = 0;
     hipError_t e = compute_units(&units);
     if (e != hipSuccess) return e;
     a.g_magic = a.G > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G) : 0;
     static bool done[kMaxDevices];
-    const auto kern = weights_kernel<T, FP8, DP, LIGHT>;
+    const auto kern = weights_kernel<T, FP8, DP, EXACT, LIGHT>;
     e = ensure_lds_limit(kern, K::LDS, done);
     if (e != hipSuccess) return e;
     if (clear_tickets && (e = launch_fill_zero(a.tickets, kPartUnits, s)) != hipSuccess) return e;
-    int grid = units * K::BLOCKS;
+    int grid = units * K::BLOCKS * (LIGHT ? 1 : kRounds);
     if (grid > kPartUnits) grid = kPartUnits;      // (a ticket to a stretch)
     a.split_chunks = (int)((int64_t)kPartUnits * 16 * a.c.D / (2 * K::Many::TOK) / grid);      // two slots of partial sums to a stretch
     if (a.split_chunks > kPartUnits / grid) a.split_chunks = kPartUnits / grid;
-    kern<<<(unsigned)grid, 256, K::LDS, s>>>(a);
+    kern<<<(unsigned)grid, K::THREADS, K::LDS, s>>>(a);
     return hipGetLastError();
 }
 
@@ -638,7 +642,8 @@ template <typename T, bool FP8, int DP> hipError_t launch_by_rows(const WeightAr
     constexpr int kMostRows = 384;
     const int64_t rows = a.c.T, seqs = a.c.S, most = rows < seqs ? rows : rows - seqs + 1;
     const bool light = rows * a.G <= kFewRows * seqs && most * a.G <= kMostRows;
-    return light ? launch<T, FP8, DP, true>(a, clear, s) : launch<T, FP8, DP, false>(a, clear, s);
+    if (light) return launch<T, FP8, DP, false, true>(a, clear, s);
+    return a.c.D == DP ? launch<T, FP8, DP, true, false>(a, clear, s) : launch<T, FP8, DP, false, false>(a, clear, s);
 }
 
 template <typename T, bool FP8> hipError_t launch_by_dim(const WeightArgs& a, bool clear, hipStream_t s)

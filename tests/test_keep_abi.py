@@ -72,6 +72,7 @@ def test_weights():
     for decay in (-0.5, 1.5, math.nan, math.inf):
         assert c.keep_status("weights", decay=decay) == SHAPE
     assert c.keep_status("weights", lse=None) == NULL and c.keep_status("weights", lse=FAKE + 2) == ALIGN
+    assert c.keep_status("weights", ldq=2 ** 23 + 8) == SHAPE
     assert c.keep_status("weights", scores=None) == NULL and c.keep_status("weights", scores=FAKE + 8) == ALIGN
 
 
