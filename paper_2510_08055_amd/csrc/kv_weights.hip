@@ -14,7 +14,6 @@ namespace {
 
 constexpr int kSeqs = 256;             // sequences that are planned at a time, a thread each
 constexpr int kFewRows = 16;           // packed rows of a sequence up to which they stay in registers
-constexpr int kRounds = 2;              // stretches of many rows to a place on a unit: the steps at a causal border take less time
 constexpr int kMinSteps = 4;           // of a stretch, where there are too few for all blocks
 
 __device__ __forceinline__ int token_of(const WeightArgs& a, int r) { return a.G == 1 ? r : (int)divided((uint32_t)r, (uint32_t)a.G, a.g_magic); }
@@ -570,8 +569,8 @@ __global__ __launch_bounds__((WeightKernel<T, FP8, DP, EXACT, LIGHT>::THREADS), 
                     while (cut(b + 1) <= x) ++b;
                     return (int)b;
                 };
-                int64_t x = cut(blockIdx.x);
-                const int64_t end = cut(blockIdx.x + 1);
+                const int64_t start = cut(blockIdx.x), end = cut(blockIdx.x + 1);
+                int64_t x = start;
                 while (x < end) {
                     const int i = found_in(plan.many, x);
                     const int64_t base = i > 0 ? plan.many[i - 1] : 0;
@@ -586,15 +585,19 @@ __global__ __launch_bounds__((WeightKernel<T, FP8, DP, EXACT, LIGHT>::THREADS), 
                         if (Many::before(st, mid) <= rem) lo = mid;
                         else hi = mid - 1;
                     }
-                    const int64_t t_begin = head_base + Many::before(st, lo), t_end = head_base + Many::before(st, lo + 1);
-                    const int64_t to = !split || t_end < end ? t_end : end;
-                    if (split || x == t_begin) {
-                        const int first = split ? owner(t_begin) : (int)blockIdx.x, last = split ? owner(t_end - 1) : first;
-                        Many::run(a, q, st, s0 + i, h, lo, (int)(x - t_begin), (int)(to - t_begin), (int)blockIdx.x - first, last - first + 1,
-                                  chunk * (int)gridDim.x + first, smem);
+                    for (int tile = lo; tile < st.end && x < end; ++tile) {
+                        const int64_t t_begin = head_base + Many::before(st, tile), t_end = head_base + Many::before(st, tile + 1);
+                        const int64_t to = !split || t_end < end ? t_end : end;
+                        if (split || x == t_begin) {
+                            int first = (int)blockIdx.x, last = first;
+                            if (split && t_begin < start) first = owner(t_begin);
+                            if (split && t_end > end) last = owner(t_end - 1);
+                            Many::run(a, q, st, s0 + i, h, tile, (int)(x - t_begin), (int)(to - t_begin), (int)blockIdx.x - first, last - first + 1,
+                                      chunk * (int)gridDim.x + first, smem);
+                            __syncthreads();
+                        }
+                        x = to;
                     }
-                    x = to;
-                    __syncthreads();
                 }
             }
         }
@@ -628,7 +631,7 @@ template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> hipError_t launc
     e = ensure_lds_limit(kern, K::LDS, done);
     if (e != hipSuccess) return e;
     if (clear_tickets && (e = launch_fill_zero(a.tickets, kPartUnits, s)) != hipSuccess) return e;
-    int grid = units * K::BLOCKS * (LIGHT ? 1 : kRounds);
+    int grid = units * K::BLOCKS;
     if (grid > kPartUnits) grid = kPartUnits;      // (a ticket to a stretch)
     a.split_chunks = (int)((int64_t)kPartUnits * 16 * a.c.D / (2 * K::Many::TOK) / grid);      // two slots of partial sums to a stretch
     if (a.split_chunks > kPartUnits / grid) a.split_chunks = kPartUnits / grid;
