@@ -317,7 +317,7 @@ moe_status moe_set_ffn_variant(moe_ctx *ctx, int32_t variant);
  * descend or leave [0, T] make moe_paged_attention compute nothing; no descriptor makes a call touch memory outside its tensors.
  * Limits (MOE_ERR_SHAPE): T * heads <= 2^30, max_pages * page <= 2^30, n_seqs < 2^22, n_pages < 2^31, and less than 2^24 blocks of 256
  * threads to a launch (attention: a block for a key/value head of a sequence that can have rows, for every 16 to 128 packed rows more, and for
- * every piece; append and gather: 16 bytes of a row to a lane, and four vectors; select: four for every sequence and key/value head, compact two).
+ * every piece; append and gather: 16 bytes of a row to a lane, and four vectors; select: four for every sequence and key/value head, compact one).
  */
 typedef enum { MOE_KV_DTYPE = 0, MOE_KV_FP8 = 1 } moe_kv_format;
 

@@ -100,6 +100,8 @@ struct CompactArgs {
     int64_t max_keep;
     int per_head;
 };
-hipError_t launch_kv_compact(int row, const CompactArgs& a, hipStream_t s);
+// words of state, zero between launches: how far the tiles of a launch are
+constexpr int kCompactWords = 1 << 16;
+hipError_t launch_kv_compact(int row, const CompactArgs& a, uint32_t* state, bool clear, hipStream_t s);
 
 }  // namespace moe

@@ -11,8 +11,8 @@ struct moe_kv_ctx {
     moe_kv_config cfg;
     float* part;
     float2* part_stats;
-    uint32_t* tickets;
-    bool tickets_clear;
+    uint32_t *tickets, *compact_state;
+    bool tickets_clear, compact_clear;      // (whether they are known to be zero)
 };
 
 namespace {
@@ -33,7 +33,7 @@ moe_status check_cfg(const moe_kv_config* c)
 
 inline size_t part_bytes(const moe_kv_config& c) { return (size_t)kPartUnits * 16 * c.dim * sizeof(float); }
 inline size_t stats_bytes() { return (size_t)kPartUnits * 16 * sizeof(float2); }
-inline size_t workspace_size(const moe_kv_config& c) { return part_bytes(c) + stats_bytes() + kPartUnits * sizeof(uint32_t); }
+inline size_t workspace_size(const moe_kv_config& c) { return part_bytes(c) + stats_bytes() + (kPartUnits + kCompactWords) * sizeof(uint32_t); }
 
 inline bool misaligned(const void* p, uintptr_t to = 16) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 inline moe_status dev(hipError_t e) { return e == hipSuccess ? MOE_OK : e == hipErrorInvalidConfiguration ? MOE_ERR_SHAPE : MOE_ERR_DEVICE; }
@@ -108,19 +108,19 @@ moe_status view_of_tokens(const moe_kv_ctx* ctx, int64_t n_pages, const moe_kv_b
 
 inline float scale2_of(const moe_kv_config& g) { return (float)(1.4426950408889634 / std::sqrt((double)g.dim)); }
 
-// A launch that uses the tickets.  They are zero between launches once they have been cleared: in front of a context's first call.  A call that is
-// being captured carries the clear along, runs when its graph is replayed, and so leaves it to the next call as well.
-template <typename F> moe_status with_tickets(moe_kv_ctx* ctx, void* stream, F launch)
+// A launch that uses counters of the workspace.  They are zero between launches once they have been cleared (is_clear): in front of a context's first
+// call.  A call that is being captured carries the clear along, runs when its graph is replayed, and so leaves it to the next call as well.
+template <typename F> moe_status with_counters(bool& is_clear, void* stream, F launch)
 {
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const bool clear = !ctx->tickets_clear;
+    const bool clear = !is_clear;
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
     if (clear && hipStreamIsCapturing(s, &capture) != hipSuccess) {
         (void)hipGetLastError();        // (the legacy stream while another one is captured)
         capture = hipStreamCaptureStatusActive;
     }
     const moe_status st = dev(launch(clear, s));
-    if (clear) ctx->tickets_clear = st == MOE_OK && capture == hipStreamCaptureStatusNone;
+    if (clear) is_clear = st == MOE_OK && capture == hipStreamCaptureStatusNone;
     return st;
 }
 
@@ -157,7 +157,7 @@ moe_status attend(moe_kv_ctx* ctx, const void* q, int64_t ldq, int64_t T, const 
     a.part = ctx->part;
     a.part_stats = ctx->part_stats;
     a.tickets = ctx->tickets;
-    return with_tickets(ctx, stream, [&](bool clear, hipStream_t s) {
+    return with_counters(ctx->tickets_clear, stream, [&](bool clear, hipStream_t s) {
         return tree ? launch_tree_attention(g.dtype, g.kv_format == MOE_KV_FP8, a, clear, s) : launch_attention(g.dtype, g.kv_format == MOE_KV_FP8, a, clear, s);
     });
 }
@@ -188,7 +188,8 @@ moe_status moe_kv_create(const moe_kv_config* cfg, void* workspace, size_t works
     c->part = static_cast<float*>(workspace);
     c->part_stats = reinterpret_cast<float2*>(static_cast<char*>(workspace) + part_bytes(*cfg));
     c->tickets = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + part_bytes(*cfg) + stats_bytes());
-    c->tickets_clear = false;
+    c->compact_state = c->tickets + kPartUnits;
+    c->tickets_clear = c->compact_clear = false;
     *out_ctx = c;
     return MOE_OK;
 }
@@ -284,7 +285,7 @@ moe_status moe_kv_weights(moe_kv_ctx* ctx, const void* q, int64_t ldq, const flo
     a.decay = opt->decay;
     a.part = ctx->part;
     a.tickets = ctx->tickets;
-    return with_tickets(ctx, stream, [&](bool clear, hipStream_t s) { return launch_kv_weights(g.dtype, g.kv_format == MOE_KV_FP8, a, clear, s); });
+    return with_counters(ctx->tickets_clear, stream, [&](bool clear, hipStream_t s) { return launch_kv_weights(g.dtype, g.kv_format == MOE_KV_FP8, a, clear, s); });
 }
 
 moe_status moe_kv_select(moe_kv_ctx* ctx, const float* scores, int64_t n_pages, const moe_kv_batch* batch, const moe_select_options* opt,
@@ -314,7 +315,7 @@ moe_status moe_kv_compact(moe_kv_ctx* ctx, const moe_kv_pages* pages, const moe_
     const moe_status st = view_of_tokens(ctx, pages->n_pages, batch, &a.c);
     if (st != MOE_OK) return st;
     if (keep->max_keep < 0 || keep->max_keep > 1 << 30 || (keep->per_head != 0 && keep->per_head != 1)) return MOE_ERR_SHAPE;
-    if (a.c.S == 0 || keep->max_keep == 0) return MOE_OK;
+    if (a.c.S == 0 || keep->max_keep == 0 || a.c.max_pages == 0) return MOE_OK;
     const moe_kv_config& g = ctx->cfg;
     const bool fp8 = g.kv_format == MOE_KV_FP8;
     if (!pages->k_pages || !pages->v_pages || (fp8 && (!pages->k_scales || !pages->v_scales)) || !keep->tokens || !keep->lens) return MOE_ERR_NULL;
@@ -331,7 +332,9 @@ moe_status moe_kv_compact(moe_kv_ctx* ctx, const moe_kv_pages* pages, const moe_
     a.first = keep->first;
     a.max_keep = keep->max_keep;
     a.per_head = keep->per_head;
-    return dev(launch_kv_compact(g.dim * (fp8 ? 1 : g.dtype == MOE_BF16 ? 2 : 4), a, static_cast<hipStream_t>(stream)));
+    return with_counters(ctx->compact_clear, stream, [&](bool clear, hipStream_t s) {
+        return launch_kv_compact(g.dim * (fp8 ? 1 : g.dtype == MOE_BF16 ? 2 : 4), a, ctx->compact_state, clear, s);
+    });
 }
 
 }  // extern "C"
