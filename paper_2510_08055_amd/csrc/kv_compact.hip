@@ -9,9 +9,15 @@
 namespace moe {
 namespace {
 
+// 16 bytes that nobody asks for again soon (16 histories: 239 us with plain stores, 215 so).
+__device__ __forceinline__ void store_stream(void* p, uint4 v)
+{
+    typedef uint32_t uint32x4_t __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(__builtin_bit_cast(uint32x4_t, v), static_cast<uint32x4_t*>(p));
+}
+
 // A tile of a list: 256 / L tokens at a time, L lanes to a row of 16-byte pieces, U times.
-constexpr int U = 4;
-template <int L> struct Tile {
+template <int L, int U> struct Tile {
     static constexpr int PER = 256 / L, TOKENS = PER * U;
     uint4 k[U], v[U];
     uint32_t ks[U], vs[U];
@@ -86,8 +92,8 @@ template <int L> struct Tile {
         for (int u = 0; u < U; ++u) {
             if (to[u] < 0) continue;
             if (piece * 16 < row) {
-                *reinterpret_cast<uint4*>(c.k + to[u] * row + piece * 16) = k[u];
-                *reinterpret_cast<uint4*>(c.v + to[u] * row + piece * 16) = v[u];
+                store_stream(c.k + to[u] * row + piece * 16, k[u]);
+                store_stream(c.v + to[u] * row + piece * 16, v[u]);
             }
             if (piece == 0 && c.ks) {
                 c.ks[to[u]] = (uint8_t)ks[u];
@@ -108,12 +114,12 @@ __device__ __forceinline__ void have_read()
 }
 
 // A block to a sequence and head, tile after tile.
-template <int L> __global__ __launch_bounds__(256) void compact_kernel(CompactArgs a, int row)
+template <int L, int U> __global__ __launch_bounds__(256) void compact_kernel(CompactArgs a, int row)
 {
     const int s = blockIdx.x / a.c.Hk, h = blockIdx.x - s * a.c.Hk;
     const int64_t count = count_of(a, s);
-    for (int64_t i = 0; i < count; i += Tile<L>::TOKENS) {
-        Tile<L> t;
+    for (int64_t i = 0; i < count; i += Tile<L, U>::TOKENS) {
+        Tile<L, U> t;
         if (!__syncthreads_or(t.find(a, s, h, i, count))) continue;
         t.read(a, row);
         have_read();
@@ -121,20 +127,21 @@ template <int L> __global__ __launch_bounds__(256) void compact_kernel(CompactAr
     }
 }
 
-// A block to a tile.  state: the next tile to draw, the blocks that have ended, then a word for every tile that has been read; zero
-// between launches: the block that ends last leaves it so.
-template <int L> __global__ __launch_bounds__(256) void compact_tiles_kernel(CompactArgs a, int row, int items, int tiles, uint32_t* state)
+// A block to a tile.  state, of each sequence and head: the next tile to draw, the blocks that have ended, then a word for every tile that has
+// been read; zero between launches: the block that ends last leaves it so.  (One pair of counters for all blocks cost 16 histories 60 us of waiting for them.)
+template <int L, int U> __global__ __launch_bounds__(256) void compact_tiles_kernel(CompactArgs a, int row, int items, int tiles, uint32_t* state)
 {
     __shared__ uint32_t drawn;
-    if (threadIdx.x == 0) drawn = __hip_atomic_fetch_add(state, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const int item = (int)(blockIdx.x % (uint32_t)items), s = item / a.c.Hk, h = item - s * a.c.Hk;
+    uint32_t* const mine = state + (int64_t)item * (tiles + 2);
+    if (threadIdx.x == 0) drawn = __hip_atomic_fetch_add(mine, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const int64_t count = count_of(a, s);
     __syncthreads();
-    const uint32_t draw = (uint32_t)__builtin_amdgcn_readfirstlane((int)drawn);
-    const int tile = (int)(draw / (uint32_t)items), item = (int)(draw - (uint32_t)tile * items);
-    const int s = item / a.c.Hk, h = item - s * a.c.Hk;
-    const int64_t count = count_of(a, s), i0 = (int64_t)tile * Tile<L>::TOKENS;
+    const int tile = __builtin_amdgcn_readfirstlane((int)drawn);
+    const int64_t i0 = (int64_t)tile * Tile<L, U>::TOKENS;
     if (i0 < count) {
-        uint32_t* read = state + 2 + (int64_t)item * tiles;
-        Tile<L> t;
+        uint32_t* const read = mine + 2;
+        Tile<L, U> t;
         const bool moves = __syncthreads_or(t.find(a, s, h, i0, count)) != 0;
         if (moves) t.read(a, row);
         have_read();
@@ -146,17 +153,21 @@ template <int L> __global__ __launch_bounds__(256) void compact_tiles_kernel(Com
             t.write(a, row);
         }
     }
-    if (threadIdx.x == 0) drawn = __hip_atomic_fetch_add(state + 1, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
-    if (drawn != gridDim.x - 1) return;
-    for (uint32_t i = threadIdx.x; i < gridDim.x + 2; i += 256) store_shared(state + i, 0u);
+    if (threadIdx.x == 0) drawn = __hip_atomic_fetch_add(mine + 1, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (drawn != (uint32_t)tiles - 1) return;
+    for (int i = threadIdx.x; i < tiles + 2; i += 256) store_shared(mine + i, 0u);
 }
 
 template <int L> hipError_t launch(const CompactArgs& a, int row, int64_t items, uint32_t* state, hipStream_t s)
 {
-    const int64_t tiles = (a.max_keep + Tile<L>::TOKENS - 1) / Tile<L>::TOKENS;
-    if (tiles == 1 || items * tiles + 2 > kCompactWords) compact_kernel<L><<<(unsigned)items, 256, 0, s>>>(a, row);
-    else compact_tiles_kernel<L><<<(unsigned)(items * tiles), 256, 0, s>>>(a, row, (int)items, (int)tiles, state);
+    // (8 times: 16 histories in tiles of 32 / 64 / 128 / 256 tokens, with one pair of counters, 412 / 239 / 181 / -, with a pair each - / 117 / 116 / 118)
+    constexpr int U = 8, TOKENS = Tile<L, U>::TOKENS;
+    const int64_t tiles = (a.max_keep + TOKENS - 1) / TOKENS;
+    if (a.max_keep <= 256 / L) compact_kernel<L, 1><<<(unsigned)items, 256, 0, s>>>(a, row);
+    else if (tiles == 1 || items * (tiles + 2) > kCompactWords) compact_kernel<L, U><<<(unsigned)items, 256, 0, s>>>(a, row);
+    else compact_tiles_kernel<L, U><<<(unsigned)(items * tiles), 256, 0, s>>>(a, row, (int)items, (int)tiles, state);
     return hipGetLastError();
 }
 
