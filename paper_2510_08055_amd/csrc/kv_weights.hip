@@ -152,7 +152,7 @@ template <typename T, bool FP8, int DP, int NJ> struct FewWeights {
 #pragma unroll
                 for (int c = 0; c < KC; ++c) {
                     const int d = c * (4 * KDIM) + g * KDIM;
-                    load_dwords<true>(p + (d < D ? d : 0) * ESZ, x.k[j][c]);
+                    load_dwords(p + (d < D ? d : 0) * ESZ, x.k[j][c]);
                 }
                 if constexpr (FP8) x.scale[j] = a.c.ks[row];
             }
@@ -338,64 +338,60 @@ template <typename T, bool FP8, int DP, bool EXACT> struct ManyWeights {
         }
     }
 
-    // Steps [x0, x1) of a tile's `count`, as piece `piece` of `pieces`; ticket: of the tile, and where piece 0 leaves its sums.
-    static __device__ __forceinline__ void run(const WeightArgs& a, const WeightSeq& q, const Steps& st, int seq, int h, int tile, int x0, int x1, int piece,
-                                               int pieces, int ticket, char* smem)
-    {
-        const int tid = here(threadIdx.x), lane = tid & 63, n = lane & 31, half = lane >> 5;
-        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const int D = EXACT ? DP : a.c.D, rows = q.n * a.G;
-        float* const lse = reinterpret_cast<float*>(smem + 2 * STAGE);
-        float* const sums = lse + 2 * ROWS;
-        int32_t* const flag = reinterpret_cast<int32_t*>(sums + TOK);
-        const int start = (int)(q.p0 + ((int64_t)tile - st.t0) * TOK);         // (from -TOK on)
-        const int j0 = start + wave * WTOK, j1 = j0 + WTOK - 1;
-        const int skip = tile > st.t0 ? (tile - st.t0) * st.less : 0;          // steps whose rows do not see the tile
-        int r0 = (int64_t)(skip + x0) * ROWS < rows ? (skip + x0) * ROWS : rows;
-        const int r1 = (int64_t)(skip + x1) * ROWS < rows ? (skip + x1) * ROWS : rows;
+    // What a block's threads need of a sequence and head to bring its rows into LDS and to take them against keys.
+    struct Rows {
+        const WeightArgs& a;
+        const WeightSeq& q;
+        int h, rows, tid, lane, n, half, wave, D;
+        uint32_t lds0;
+        float* lse;
 
-        // A stage's rows go straight into LDS, chunk c of row r to place c ^ swz(r).  A load has AT of them: where they are of one token, or of whole
-        // tokens, only its address goes on from load to load; else, and where there are no more rows (the last one stands for them), every lane finds its own.
-        // (Rows of a load lie within 2^31 bytes: the launch sees to it.)
-        const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_address(smem));
-        const int stride = (int)a.ldq * (int)sizeof(T), rowb = D * (int)sizeof(T);
-        const bool even = a.G % AT == 0 || AT % a.G == 0;
-        constexpr int PER = ROWS / WAVES;        // rows of a wave's lse
-        auto aim = [&](int r, int tok0, int chunk) {
-            const int rr = r < rows ? r : rows - 1, tok = token_of(a, rr);
-            // (chunks past the dimension: no product reads them)
-            return (uint32_t)((tok - tok0) * stride + (rr - tok * a.G) * rowb + (chunk * 16 < rowb ? chunk * 16 : 0));
-        };
-        const uint32_t lane_off = (uint32_t)(a.G % AT == 0 ? lane / CH * rowb : lane / CH / a.G * stride + lane / CH % a.G * rowb);
-        auto fetch = [&](int first, int slot) {
-            const bool all = even && first + ROWS <= rows;
+        __device__ __forceinline__ Rows(const WeightArgs& a_, const WeightSeq& q_, int h_, char* smem) : a(a_), q(q_), h(h_)
+        {
+            tid = here(threadIdx.x);
+            lane = tid & 63;
+            n = lane & 31;
+            half = lane >> 5;
+            wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+            D = EXACT ? DP : a.c.D;
+            rows = q.n * a.G;
+            lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_address(smem));
+            lse = reinterpret_cast<float*>(smem + 2 * STAGE);
+        }
+
+        // Rows `first` on into a slot, straight into LDS, chunk c of row r to place c ^ swz(r).  A load has AT of them: where they are of one token, or of
+        // whole tokens, only its address goes on from load to load; else, and where there are no more rows (the last one stands for them), every lane
+        // finds its own.  (Rows of a load lie within 2^31 bytes: the launch sees to it.)
+        __device__ __forceinline__ void fetch(int first, int slot) const
+        {
+            const int stride = (int)a.ldq * (int)sizeof(T), rowb = D * (int)sizeof(T);
+            const bool all = (a.G % AT == 0 || AT % a.G == 0) && first + ROWS <= rows;
+            const uint32_t lane_off = (uint32_t)(a.G % AT == 0 ? lane / CH * rowb : lane / CH / a.G * stride + lane / CH % a.G * rowb);
+            auto aim = [&](int r, int tok0) {
+                const int rr = r < rows ? r : rows - 1, tok = token_of(a, rr);
+                return (uint32_t)((tok - tok0) * stride + (rr - tok * a.G) * rowb);
+            };
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
                 const int lr = (wave * LOADS + i) * AT, r = first + lr;
                 const int rr = r < rows ? r : rows - 1, tok = token_of(a, rr);
                 const int chunk = (lane % CH) ^ swz(lr + lane / CH);
                 const char* base = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (int64_t)(q.row0 + tok) * a.ldq + (int64_t)h * a.G * D);
-                const uint32_t off[1] = {all ? lane_off + (chunk * 16 < rowb ? chunk * 16 : 0) : aim(r + lane / CH, tok, chunk)};
+                // (chunks past the dimension: no product reads them)
+                const uint32_t off[1] = {(all ? lane_off : aim(r + lane / CH, tok)) + (chunk * 16 < rowb ? chunk * 16 : 0)};
                 load_lds_group(off, all ? base + (r - tok * a.G) * rowb : base, lds0 + slot * STAGE + lr * ROWB);
             }
+            constexpr int PER = ROWS / WAVES;        // rows of a wave's lse
             if (lane < PER) {
                 const int r = first + wave * PER + lane, rr = r < rows ? r : rows - 1, tok = token_of(a, rr), tok0 = token_of(a, first);
                 load_lds_dword((uint32_t)((tok - tok0) * a.Hq + rr - tok * a.G) * 4, reinterpret_cast<const char*>(a.lse + (int64_t)(q.row0 + tok0) * a.Hq + h * a.G),
                                lds0 + 2 * STAGE + (slot * ROWS + wave * PER) * 4);
             }
-        };
-        if (r0 < r1) fetch(r0, 0);
-        Keys K;
-        {
-            const int64_t row = place_of(a, q, seq, h, j0 + n);
-            load_keys(a, row < 0 ? 0 : row, half, K);      // (a token that is not there: some row, its sum is not stored)
         }
-        float acc[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[i] = 0;
 
-        // 32 rows of a stage with the wave's tokens
-        auto product = [&](int slot, int part) {
+        // 32 rows of a slot with the wave's tokens
+        __device__ __forceinline__ float16_t product(const Keys& K, int slot, int part) const
+        {
             const uint32_t at = lds0 + slot * STAGE + (part * 32 + n) * ROWB + ((half ^ swz(n)) * 16);
             float16_t x = float16_t{};
 #pragma unroll
@@ -411,16 +407,15 @@ template <typename T, bool FP8, int DP, bool EXACT> struct ManyWeights {
                 }
             }
             return x;
-        };
-        int slot = 0;
-        for (; r0 < r1; r0 += ROWS, slot ^= 1) {
-            wait_vmcnt<0>();
-            block_barrier();
-            if (r0 + ROWS < r1) fetch(r0 + ROWS, slot ^ 1);
-            if (j0 >= q.held) continue;
+        }
+
+        // Adds the weights of a slot's rows, r0 and the ROWS - 1 after it, to the sums of tokens j0 .. j0 + 31.
+        __device__ __forceinline__ void add(const Keys& K, int slot, int r0, int j0, float (&acc)[16]) const
+        {
             const float* const l = lse + slot * ROWS;
+            const int j1 = j0 + WTOK - 1;
             const int p_first = q.p0 + token_of(a, r0), r_last = r0 + ROWS <= rows ? r0 + ROWS - 1 : rows - 1, p_last = q.p0 + token_of(a, r_last);
-            if (a.causal && p_last < j0) continue;                             // (no row sees a token of the wave)
+            if (a.causal && p_last < j0) return;                                   // (no row sees a token of the wave)
             bool none = false;
 #pragma unroll
             for (int i = 0; i < ROWS; i += 64) none |= l[i + lane] == -__builtin_inff();
@@ -429,11 +424,11 @@ template <typename T, bool FP8, int DP, bool EXACT> struct ManyWeights {
 #pragma unroll 1
                 for (int part = 0; part < PARTS; ++part) {
                     const float l2 = l[part * 32 + n] * kLog2e;
-                    const float16_t x = product(slot, part);
+                    const float16_t x = product(K, slot, part);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) acc[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale2, -l2));
                 }
-                continue;
+                return;
             }
 #pragma unroll 1
             for (int part = 0; part < PARTS; ++part) {
@@ -443,8 +438,8 @@ template <typename T, bool FP8, int DP, bool EXACT> struct ManyWeights {
                 if ((a.causal && q.p0 + token_of(a, last) < j0) || (a.window > 0 && q.p0 + token_of(a, first) - a.window + 1 > j1)) continue;
                 const int r = first + n, p = q.p0 + token_of(a, r < rows ? r : rows - 1);
                 const float raw = l[part * 32 + n], l2 = raw * kLog2e;
-                const int see_hi = raw == -__builtin_inff() || r >= rows ? start : a.causal ? p + 1 : 0x7fffffff, see_lo = a.window > 0 ? p - a.window + 1 : -0x7fffffff;
-                const float16_t x = product(slot, part);
+                const int see_hi = raw == -__builtin_inff() || r >= rows ? j0 : a.causal ? p + 1 : 0x7fffffff, see_lo = a.window > 0 ? p - a.window + 1 : -0x7fffffff;
+                const float16_t x = product(K, slot, part);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int j = j0 + (i / 4) * 8 + 4 * half + i % 4;
@@ -454,17 +449,49 @@ template <typename T, bool FP8, int DP, bool EXACT> struct ManyWeights {
             }
         }
 
-        // over the 32 columns; lane n keeps the sum of the token whose number is n's
-        float mine = 0;
+        // Sums over the 32 columns: in lanes n < 16, that of token (n / 4) * 8 + 4 half + n % 4.
+        __device__ __forceinline__ float total(const float (&acc)[16]) const
+        {
+            float mine = 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float v = over_sixteen(acc[i]);
-            mine = (n & 15) == i ? v : mine;
+            for (int i = 0; i < 16; ++i) {
+                const float v = over_sixteen(acc[i]);
+                mine = (n & 15) == i ? v : mine;
+            }
+            const auto other = __builtin_amdgcn_permlane16_swap(__float_as_uint(mine), __float_as_uint(mine), false, false);
+            return __uint_as_float(other[0]) + __uint_as_float(other[1]);
         }
-        const auto other = __builtin_amdgcn_permlane16_swap(__float_as_uint(mine), __float_as_uint(mine), false, false);
-        if (n < 16) sums[wave * WTOK + (n / 4) * 8 + 4 * half + n % 4] = __uint_as_float(other[0]) + __uint_as_float(other[1]);
+        __device__ __forceinline__ int token() const { return (n / 4) * 8 + 4 * half + n % 4; }
+    };
+
+    // Steps [x0, x1) of a tile's `count`, as piece `piece` of `pieces`; ticket: of the tile, and where piece 0 leaves its sums.
+    static __device__ __forceinline__ void run(const WeightArgs& a, const WeightSeq& q, const Steps& st, int seq, int h, int tile, int x0, int x1, int piece,
+                                               int pieces, int ticket, char* smem)
+    {
+        const Rows R(a, q, h, smem);
+        float* const sums = R.lse + 2 * ROWS;
+        int32_t* const flag = reinterpret_cast<int32_t*>(sums + TOK);
+        const int start = (int)(q.p0 + ((int64_t)tile - st.t0) * TOK);         // (from -TOK on)
+        const int j0 = start + R.wave * WTOK;
+        const int skip = tile > st.t0 ? (tile - st.t0) * st.less : 0;          // steps whose rows do not see the tile
+        int r0 = (int64_t)(skip + x0) * ROWS < R.rows ? (skip + x0) * ROWS : R.rows;
+        const int r1 = (int64_t)(skip + x1) * ROWS < R.rows ? (skip + x1) * ROWS : R.rows;
+        if (r0 < r1) R.fetch(r0, 0);
+        Keys K;
+        const int64_t row = place_of(a, q, seq, h, j0 + R.n);
+        load_keys(a, row < 0 ? 0 : row, R.half, K);      // (a token that is not there: some row, its sum is not stored)
+        float acc[16] = {};
+        int slot = 0;
+        for (; r0 < r1; r0 += ROWS, slot ^= 1) {
+            wait_vmcnt<0>();
+            block_barrier();
+            if (r0 + ROWS < r1) R.fetch(r0 + ROWS, slot ^ 1);
+            if (j0 < q.held) R.add(K, slot, r0, j0, acc);
+        }
+        const float mine = R.total(acc);
+        if (R.n < 16) sums[R.wave * WTOK + R.token()] = mine;
         __syncthreads();
-        const int j = start + tid;
+        const int tid = R.tid, j = start + tid;
         float w = tid < TOK ? sums[tid] : 0.0f;
         if (pieces > 1) {
             const int own = piece == 0 ? 2 * ticket + 1 : 2 * (ticket + piece);
@@ -481,11 +508,45 @@ template <typename T, bool FP8, int DP, bool EXACT> struct ManyWeights {
             if (at >= 0) store_score(a, q, at, j, w);
         }
     }
+
+    // ---- sequences whose rows fit both slots: brought there once, they meet all tokens of a stretch; every wave for itself ----
+    static __device__ __forceinline__ bool fit(const WeightArgs& a, const WeightSeq& q) { return (int64_t)q.n * a.G <= 2 * ROWS; }
+    static __device__ __forceinline__ int units(const WeightSeq& q) { return q.held > 0 ? (q.held - (q.lo & ~(WTOK - 1)) + WTOK - 1) / WTOK : 0; }
+    // Tokens [begin, end) of a sequence and head, begin a multiple of 32.
+    static __device__ __forceinline__ void run_held(const WeightArgs& a, const WeightSeq& q, int seq, int h, int begin, int end, char* smem)
+    {
+        const Rows R(a, q, h, smem);
+        R.fetch(0, 0);
+        if (R.rows > ROWS) R.fetch(ROWS, 1);
+        Entries pages;
+        const int shift = a.c.page_shift, mask = (1 << shift) - 1;
+        auto keys_at = [&](int j0) {
+            const int j = j0 + R.n, id = __shfl(pages.id, (j >> shift) - pages.base);
+            return id < 0 ? (int64_t)0 : page_row(id, a.c.Hk, h, shift, j & mask);
+        };
+        const int first = begin + R.wave * WTOK;
+        if (first < end) pages.hold(a.c, seq, first >> shift, end);
+        wait_vmcnt<0>();
+        block_barrier();
+        for (int j0 = first; j0 < end; j0 += TOK) {
+            if (((j0 + WTOK - 1) >> shift) - pages.base >= 64) pages.hold(a.c, seq, j0 >> shift, end);
+            Keys K;
+            load_keys(a, keys_at(j0), R.half, K);
+            // (the score's place and what it was, on the way beside the keys)
+            const int j = j0 + R.token(), id = __shfl(pages.id, ((R.n < 16 ? j : j0) >> shift) - pages.base);
+            const int64_t at = R.n < 16 && id >= 0 && j >= q.lo && j < end ? page_row(id, a.c.Hk, h, shift, j & mask) : -1;
+            const float old = at >= 0 && j < q.p0 && a.decay != 0.0f ? a.scores[at] : 0.0f;
+            float acc[16] = {};
+            for (int slot = 0; slot * ROWS < R.rows; ++slot) R.add(K, slot, slot * ROWS, j0, acc);
+            const float w = R.total(acc);
+            if (at >= 0) a.scores[at] = __builtin_fmaf(a.decay, old, w);
+        }
+    }
 };
 
 struct WeightPlan {
-    int64_t few[kSeqs], many[kSeqs];   // units and steps of the sequences up to and with each
-    int64_t sums[2][8];
+    int64_t few[kSeqs], held[kSeqs], many[kSeqs];      // units and steps of the sequences up to and with each
+    int64_t sums[3][8];
 };
 
 __device__ __forceinline__ int64_t scan64(int64_t v)
@@ -514,7 +575,7 @@ template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> struct WeightKer
     typedef FewWeights<T, FP8, DP, F32 || (!LIGHT && DP > 64) ? 1 : 2> Few;
     typedef ManyWeights<T, FP8, DP, EXACT> Many;
     static constexpr int THREADS = LIGHT ? 256 : 64 * Many::WAVES;
-    static constexpr int BLOCKS = LIGHT ? (DP > 128 ? (F32 ? 1 : 2) : DP > 64 ? (F32 ? 2 : 3) : F32 ? 3 : 4) : DP > 128 || (F32 && DP > 64) ? 1 : 2;      // of a unit
+    static constexpr int BLOCKS = LIGHT ? (DP > 128 ? 1 : DP > 64 ? (FP8 ? (F32 ? 2 : 3) : 2) : F32 ? 3 : 4) : DP > 128 || (F32 && DP > 64) ? 1 : 2;      // of a unit
     static constexpr size_t PLAN_AT = LIGHT ? 0 : (Many::LDS + 15) / 16 * 16, LDS = PLAN_AT + sizeof(WeightPlan);
 };
 template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT>
@@ -529,29 +590,39 @@ __global__ __launch_bounds__((WeightKernel<T, FP8, DP, EXACT, LIGHT>::THREADS), 
     const int Hk = a.c.Hk;
     for (int s0 = 0; s0 < a.c.S; s0 += kSeqs) {
         const int s = s0 + threadIdx.x;
-        int64_t few = 0, many = 0;
+        int64_t few = 0, held = 0, many = 0;
         if (threadIdx.x < kSeqs && s < a.c.S) {
             const WeightSeq q = seq_of(a, s);
             if (LIGHT || q.n * a.G <= kFewRows) {
                 few = (int64_t)Few::units(q) * Hk;
             } else if constexpr (!LIGHT) {
-                const Steps st = Many::steps_of(a, q);
-                many = Many::before(st, st.end) * Hk;
+                if (Many::fit(a, q)) {
+                    held = (int64_t)Many::units(q) * Hk;
+                } else {
+                    const Steps st = Many::steps_of(a, q);
+                    many = Many::before(st, st.end) * Hk;
+                }
             }
         }
         few = scan64(few);
-        many = scan64(many);
+        if constexpr (!LIGHT) {
+            held = scan64(held);
+            many = scan64(many);
+        }
         if (lane == 63) {
             plan.sums[0][wave] = few;
-            plan.sums[1][wave] = many;
+            plan.sums[1][wave] = held;
+            plan.sums[2][wave] = many;
         }
         __syncthreads();
         for (int w = 0; w < wave; ++w) {
             few += plan.sums[0][w];
-            many += plan.sums[1][w];
+            held += plan.sums[1][w];
+            many += plan.sums[2][w];
         }
         if (threadIdx.x < kSeqs) {
             plan.few[threadIdx.x] = few;
+            plan.held[threadIdx.x] = held;
             plan.many[threadIdx.x] = many;
         }
         __syncthreads();
@@ -601,6 +672,28 @@ __global__ __launch_bounds__((WeightKernel<T, FP8, DP, EXACT, LIGHT>::THREADS), 
                 }
             }
         }
+        // a sequence's and head's tokens from unit `from` to `to`
+        auto span = [](const WeightSeq& q, int tok, int from, int to, int& begin, int& end) {
+            begin = (q.lo & ~(tok - 1)) + from * tok;
+            end = begin + (to - from) * tok < q.held ? begin + (to - from) * tok : q.held;
+        };
+        if constexpr (!LIGHT) {
+            const int64_t all = plan.held[kSeqs - 1];
+            int64_t x = blockIdx.x * all / gridDim.x;
+            const int64_t end = (blockIdx.x + 1) * all / gridDim.x;
+            while (x < end) {
+                const int i = found_in(plan.held, x);
+                const int64_t base = i > 0 ? plan.held[i - 1] : 0;
+                const WeightSeq q = seq_of(a, s0 + i);
+                const int units = Many::units(q), h = (int)((x - base) / units), from = (int)(x - base - (int64_t)h * units);
+                const int to = end - x < units - from ? from + (int)(end - x) : units;
+                int begin, stop;
+                span(q, Many::WTOK, from, to, begin, stop);
+                Many::run_held(a, q, s0 + i, h, begin, stop, smem);
+                __syncthreads();
+                x += to - from;
+            }
+        }
         const int64_t all = plan.few[kSeqs - 1], waves = (int64_t)gridDim.x * (K::THREADS / 64), me = (int64_t)blockIdx.x * (K::THREADS / 64) + wave;
         int64_t x = me * all / waves;
         const int64_t end = (me + 1) * all / waves;
@@ -610,9 +703,9 @@ __global__ __launch_bounds__((WeightKernel<T, FP8, DP, EXACT, LIGHT>::THREADS), 
             const WeightSeq q = seq_of(a, s0 + i);
             const int units = Few::units(q), h = (int)((x - base) / units), from = (int)(x - base - (int64_t)h * units);
             const int to = end - x < units - from ? from + (int)(end - x) : units;
-            const int start = q.lo & ~(Few::TOK - 1);
-            const int stop = start + to * Few::TOK < q.held ? start + to * Few::TOK : q.held;
-            Few::run(a, q, s0 + i, h, start + from * Few::TOK, stop);
+            int begin, stop;
+            span(q, Few::TOK, from, to, begin, stop);
+            Few::run(a, q, s0 + i, h, begin, stop);
             x += to - from;
         }
         __syncthreads();
