@@ -342,3 +342,105 @@ def test_a_verified_draft_is_a_chain(gpu_lib):
     # and the cache holds what appending the chain would have left
     k, v = ctx.moe_kv_gather(pages, chain, T=4)
     assert torch.equal(k, b.k[path]) and torch.equal(v, b.v[path])
+
+
+@pytest.mark.parametrize("dtype,group", [(torch.bfloat16, 8), (torch.bfloat16, 5), (torch.float32, 4)])
+def test_weights_of_rows_at_the_edges_of_stages(gpu_lib, dtype, group):
+    """Rows that are kept in registers, those that LDS holds, and more; one to three stages of them, whole and with a rest."""
+    edges = [1, 2, 3, 4, 12, 13, 16, 17, 24, 25, 26, 31, 32, 33, 51, 52, 63, 64, 65, 96, 97, 103]
+    check_weights(gpu_lib, Batch(edges, [n + 37 * i % 500 for i, n in enumerate(edges)], 2 * group, 2, 64, 16, dtype, seed=group))
+    check_weights(gpu_lib, Batch([33, 64, 96], [3000, 64, 2000], group, 1, 128, 64, dtype, "fp8", seed=group), window=200, decay=0.25)
+
+
+def test_weights_of_long_prompts(gpu_lib):
+    """Tiles that many stretches share, behind a prompt's start and a history; beside decode and held rows."""
+    for dtype, fmt, dim in ((torch.bfloat16, "", 128), (torch.bfloat16, "fp8", 64), (torch.float32, "", 64)):
+        rows, kv = [1500, 1, 20, 700], [1500, 2000, 900, 3100]
+        b = Batch(rows, kv, 8, 2, dim, 16, dtype, fmt, seed=dim)
+        check_weights(gpu_lib, b)
+        check_weights(gpu_lib, b, window=333, decay=0.5)
+        check_weights(gpu_lib, b, causal=False, decay=0.0)
+
+
+def test_weights_of_more_sequences_than_have_slots(gpu_lib):
+    """Prompts in the first and the last of 2400 sequences: the last ones' tiles have no slots for partial sums and are not shared."""
+    S = 2400
+    rows = [1] * S
+    for s in (0, 1, 255, 256, 1000, 2047, 2048, 2300, S - 1):
+        rows[s] = 150
+    kv = [n + (200 if n > 1 else s % 7) for s, n in enumerate(rows)]
+    check_weights(gpu_lib, Batch(rows, kv, 4, 1, 16, 16, seed=1))
+
+
+def graphed(f):
+    """f captured: a function that replays it.  Its first call runs in the graph, so what a context clears belongs to it."""
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        f()
+    return g.replay
+
+
+@pytest.mark.parametrize("warm", [False, True])
+def test_captured_calls_replay(gpu_lib, warm):
+    """A pass of all calls in a graph, replayed over new descriptors with eager calls of the same context and waits between."""
+    b = Batch([30, 300, 1, 8], [200, 900, 500, 70], 8, 2, 64, 16, seed=40)
+    ctx, pages, batch = b.context(gpu_lib)
+    parents = torch.tensor([i - 1 if n > 64 else (i - 1) // 2 for n in b.rows for i in range(n)], dtype=torch.int32, device=DEV)
+    lse, out = torch.empty(b.T, 8, device=DEV), torch.empty(b.T, 8, 64, dtype=torch.bfloat16, device=DEV)
+    scores = scores_of(b)
+    masks, positions = torch.empty(b.T, 1, dtype=torch.int64, device=DEV), torch.empty(b.T, dtype=torch.int32, device=DEV)
+    keep, lens = torch.empty(4, 2, 150, dtype=torch.int32, device=DEV), torch.empty(4, dtype=torch.int32, device=DEV)
+    start = [t.clone() for t in (b.k_pages, b.v_pages, scores)]
+
+    def calls():
+        ctx.moe_tree_masks(parents, batch, masks=masks, positions=positions)
+        ctx.moe_tree_attention(b.q, pages, batch, masks, out=out)
+        ctx.moe_paged_attention(b.q, pages, batch, lse=lse)
+        ctx.moe_kv_weights(b.q, lse, pages, batch, scores)
+        ctx.moe_kv_select(scores, batch, 150, first=2, recent=70, keep=keep, keep_lens=lens)
+        ctx.moe_kv_compact(pages, batch, keep, lens, scores=scores)
+
+    def reset():
+        for t, w in zip((b.k_pages, b.v_pages, scores), start):
+            t.copy_(w)
+
+    def results():
+        return [bits(t).clone() for t in (masks, positions, out, scores, keep, lens, b.k_pages, b.v_pages)]
+
+    if warm:
+        calls()
+        torch.cuda.synchronize()
+    replay = graphed(calls)
+    for i, kv in enumerate(([200, 900, 500, 70], [31, 300, 2, 9], [180, 880, 512, 64], [200, 900, 500, 70])):
+        b.kv_lens.copy_(torch.tensor(kv, dtype=torch.int32))
+        reset()
+        replay()
+        got = results()
+        reset()
+        calls()
+        for x, y in zip(got, results()):
+            assert torch.equal(x, y), i
+        torch.cuda.synchronize()
+
+
+def test_calls_on_another_stream(gpu_lib):
+    """A context's calls follow the current stream."""
+    b = Batch([40, 1, 200], [300, 700, 200], 8, 2, 64, 16, seed=41)
+    ctx, pages, batch = b.context(gpu_lib)
+    lse = torch.empty(b.T, 8, device=DEV)
+    ctx.moe_paged_attention(b.q, pages, batch, lse=lse)
+    want = ctx.moe_kv_weights(b.q, lse, pages, batch, scores_of(b))
+    keep, lens = ctx.moe_kv_select(want, batch, 100, recent=10)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        scores = scores_of(b)
+        for _ in range(3):
+            late = torch.randn(2048, 2048, device=DEV) @ torch.randn(2048, 2048, device=DEV)
+        scores += 0.0 * late[0, 0].nan_to_num()
+        got = ctx.moe_kv_weights(b.q, lse, pages, batch, scores)
+        keep2, lens2 = ctx.moe_kv_select(got, batch, 100, recent=10)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got.nan_to_num(-1.0), want.nan_to_num(-1.0)) and torch.equal(keep, keep2) and torch.equal(lens, lens2)
