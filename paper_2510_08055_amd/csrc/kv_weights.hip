@@ -14,7 +14,7 @@ namespace {
 
 constexpr int kSeqs = 256;             // sequences that are planned at a time, a thread each
 constexpr int kFewRows = 16;           // packed rows of a sequence up to which they stay in registers
-constexpr int kMinSteps = 4;           // of a stretch, where there are too few for all blocks
+constexpr int kMinSteps = 2;           // of a stretch, where there are too few for all blocks (512 rows in groups of 8, us, 1 / 2 / 4: 25.8 / 26.1 / 32.7)
 
 __device__ __forceinline__ int token_of(const WeightArgs& a, int r) { return a.G == 1 ? r : (int)divided((uint32_t)r, (uint32_t)a.G, a.g_magic); }
 

@@ -76,6 +76,16 @@ def test_weights_of_many_sequences(gpu_lib, S):
     check_weights(gpu_lib, Batch(rows, kv, 4, 2, 64, 16, seed=S))
 
 
+@pytest.mark.parametrize("dtype,fmt,dim", [(torch.bfloat16, "", 128), (torch.bfloat16, "fp8", 64), (torch.float32, "", 64), (torch.bfloat16, "", 256)])
+def test_weights_of_a_draft_among_decode_rows(gpu_lib, dtype, fmt, dim):
+    """More rows than the registers hold at once, in a batch that is one of few rows on average."""
+    rows, kv = [1] * 40 + [20] + [1] * 23 + [3], [17 * i % 300 + 1 for i in range(40)] + [333] + [90] * 23 + [3]
+    b = Batch(rows, kv, 8, 2, dim, 16, dtype, fmt, seed=dim)
+    check_weights(gpu_lib, b)
+    check_weights(gpu_lib, b, window=30, decay=0.5)
+    check_weights(gpu_lib, b, causal=False, decay=0.0)
+
+
 def test_weights_where_nothing_is_seen(gpu_lib):
     """No tokens; fewer tokens than rows; pages given back; a table that ends early; rows whose lse is minus infinity."""
     b = Batch([2, 5, 1, 2, 3], [0, 2, 40, 100, 90], 4, 2, 64, 16, seed=11, dropped=((2, 0), (2, 1), (2, 2), (3, 5), (3, 6), (4, 2), (4, 3)))
