@@ -1,11 +1,20 @@
 // The attention weight that cached tokens receive: column sums of exp(q . k / sqrt(dim) - lse), without the matrix they are sums of.
 //
 // Scores are computed transposed as in the attention, S = K Q^T, a query row to a lane's column: a row's lse is lane-local, and the sums of the
-// exponentials over the rows stay in the lanes until the end.  There are two bodies: for sequences of few rows the rows stay in registers and the keys
-// stream by (read once: that bounds it); for many rows the keys of 64 tokens stay in a wave's registers and the rows pass by.
+// exponentials over the rows stay in the lanes until the end.  There are three ways to bring rows and keys together, by the packed rows of a sequence:
+//   up to 16: the rows stay in registers, and the keys stream by, read once, which bounds it.  64 rows over up to 8192 tokens, 188 MB of keys, 43.5 us,
+//     4.4 TB/s (a copy of 4 GiB 4.8).  Keys are plain loads: an instruction takes half a line of each row (as a stream 54 -> 57 us).
+//   up to what LDS holds (256; fp32 128): the rows stay there, and every wave takes 32 tokens' keys for itself, with no barrier until the end.
+//     What bounds it: VALU, and the chain page table, keys, products of each 32 tokens.  32 rows of 64 heads over up to 16384 FP8 tokens in 12 sequences
+//     46 us (61 as more rows are taken).
+//   more: a block holds 256 tokens' keys, 32 to a wave, and takes the rows that see them 128 at a time from LDS, brought there by direct
+//     loads while the 128 before are used.  What bounds it: a prompt of 8192 rows and 32 heads, dim 128, takes 350 us (0.79 PFLOP/s); VALU busy 54 % and the matrix pipes
+//     32 % of them, with four waves to a SIMD; waves wait 44 % of their cycles, most of that for products that follow each other and for LDS (300 us with no rows brought).
+//     Fewer waves with more each were slower: 64 tokens to a wave 440 to 500 us, and with the products of one half of them beside the exponentials of the other,
+//     scheduled by hand, 445 (two waves to a SIMD) and 610 (one); stages of 64 rows, four in flight, 380; neighbouring stretches on one XCD 367.
 //
-// Work is cut on the device, from the descriptors, into equal stretches: of 32-token units of all sequences and heads, a stretch to a wave, where rows are
-// few; where they are many, of steps (128 packed rows by 256 tokens), a stretch to a block.  A token's sum belongs to one wave, or is joined from the
+// Work is cut on the device, from the descriptors, into equal stretches: of units of 16 or 32 tokens of all sequences and heads, a stretch to a wave or a
+// block; of steps (128 packed rows by 256 tokens) where rows are many, a stretch to a block.  A token's sum belongs to one wave, or is joined from the
 // stretches that its tokens' steps fall into, in their order, by the block that ends the last: there are no atomic sums, and a batch's result is always the same bits.
 #include "attention_tile.h"
 
@@ -259,7 +268,7 @@ struct Steps {
     int less;                          // by which each tile from t0 on has its rows start later (causal)
     int each;                          // steps of a tile, where they are the same for all; 0: all rows from the first that sees it
 };
-// EXACT: the heads are DP wide, no less.
+// EXACT: the heads are DP wide, no less.  ROWS: what 64 KB of LDS hold in two slots at dim 128, so that two blocks share a unit.
 template <typename T, bool FP8, int DP, bool EXACT> struct ManyWeights {
     static constexpr bool F32 = sizeof(T) == 4;
     static constexpr int WAVES = 8, WTOK = 32, TOK = WAVES * WTOK;         // tokens of a wave, of a block
@@ -575,6 +584,8 @@ template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> struct WeightKer
     typedef FewWeights<T, FP8, DP, F32 || (!LIGHT && DP > 64) ? 1 : 2> Few;
     typedef ManyWeights<T, FP8, DP, EXACT> Many;
     static constexpr int THREADS = LIGHT ? 256 : 64 * Many::WAVES;
+    // (64 decode rows over up to 8192 tokens, us, light blocks of a unit as here / one more: bf16 dim 128 44 / 54, 256 80 / 119, fp32 30 / -; / one fewer: bf16 64 47 / 51 with two
+    // fewer, FP8 128 27 / 29)
     static constexpr int BLOCKS = LIGHT ? (DP > 128 ? 1 : DP > 64 ? (FP8 ? (F32 ? 2 : 3) : 2) : F32 ? 3 : 4) : DP > 128 || (F32 && DP > 64) ? 1 : 2;      // of a unit
     static constexpr size_t PLAN_AT = LIGHT ? 0 : (Many::LDS + 15) / 16 * 16, LDS = PLAN_AT + sizeof(WeightPlan);
 };
