@@ -291,7 +291,7 @@ template <typename T, bool FP8, int DP, bool EXACT> struct ManyWeights {
         Steps s{0, 0, 0, 0, 0, 0};
         if (q.held == 0) return s;
         s.total = (int)(((int64_t)q.n * a.G + ROWS - 1) / ROWS);
-        s.t0 = q.p0 > 0 ? (q.p0 + TOK - 1) / TOK : 0;
+        s.t0 = q.p0 > 0 ? (int)(((int64_t)q.p0 + TOK - 1) / TOK) : 0;
         const int64_t start = q.p0 - (int64_t)s.t0 * TOK;      // of tile 0: at most 0
         s.end = (int)((q.held - start + TOK - 1) / TOK);
         s.first = (int)((q.lo - start) / TOK);

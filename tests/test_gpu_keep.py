@@ -104,6 +104,22 @@ def test_weights_where_nothing_is_seen(gpu_lib):
     assert (got[~torch.isnan(got)] == 0).all()
 
 
+@pytest.mark.parametrize("last", [2 ** 31 - 1, 2 ** 31 - 255, 2 ** 31 - 256, 2 ** 30 + 77])
+def test_weights_of_lengths_past_the_table(gpu_lib, last):
+    """Positions come from the lengths as they are: rows far behind what the table reaches see all of that, or, with a window, nothing."""
+    for dtype, fmt in ((torch.bfloat16, ""), (torch.float32, "fp8")):
+        b = Batch([3, 40, 150], [300, 300, 300], 8, 2, 64, 16, dtype, fmt, seed=5)
+        b.kv = [last, last, 5000]
+        b.kv_lens.copy_(torch.tensor(b.kv, dtype=torch.int32))
+        lse = torch.randn(b.T, 8, device=DEV) + 6
+        scores = torch.rand(b.k_pages.shape[0], 2, 16, device=DEV)
+        b.k_pages = torch.where(torch.isnan(b.k_pages.float()), torch.zeros_like(b.k_pages.float()), b.k_pages.float()).to(b.k_pages.dtype)
+        if b.k_scales is not None:
+            b.k_scales[b.k_scales == 255] = 127
+        for causal, window, decay in ((True, 0, 1.0), (False, 0, 0.5), (True, 500, 0.5), (True, 2 ** 30, 0.0)):
+            check_weights(gpu_lib, b, causal, window, decay, lse=lse, scores=scores)
+
+
 def test_weights_of_a_token_are_its_own(gpu_lib):
     """A key that is not finite reaches its own sum alone, a row that is not finite those of the tokens that it sees, and with decay 0 no
     earlier score is read."""
