@@ -76,12 +76,14 @@ struct WeightArgs {
     int64_t ldq;
     int Hq, G, causal, window;
     uint32_t g_magic;              // (set by the launch, as is:)
+    int few_rows;                  // packed rows of the sequences that the kernel of few rows takes
     int split_chunks;              // of 256 sequences, for whose partial sums there are slots
     float scale2, decay;
     float* part;                   // partial sums of tokens, and tickets, as in AttnArgs
     uint32_t* tickets;
 };
-hipError_t launch_kv_weights(int dtype, bool fp8, const WeightArgs& a, bool clear_tickets, hipStream_t s);
+// clear_tickets: as above; false again where the tickets were not needed, and so not cleared
+hipError_t launch_kv_weights(int dtype, bool fp8, const WeightArgs& a, bool& clear_tickets, hipStream_t s);
 
 // kv_select.hip
 struct SelectArgs {

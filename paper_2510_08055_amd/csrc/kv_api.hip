@@ -110,10 +110,11 @@ inline float scale2_of(const moe_kv_config& g) { return (float)(1.44269504088896
 
 // A launch that uses counters of the workspace.  They are zero between launches once they have been cleared (is_clear): in front of a context's first
 // call.  A call that is being captured carries the clear along, runs when its graph is replayed, and so leaves it to the next call as well.
+// (launch may say that it did not clear them: bool&.)
 template <typename F> moe_status with_counters(bool& is_clear, void* stream, F launch)
 {
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const bool clear = !is_clear;
+    bool clear = !is_clear;
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
     if (clear && hipStreamIsCapturing(s, &capture) != hipSuccess) {
         (void)hipGetLastError();        // (the legacy stream while another one is captured)
@@ -285,7 +286,7 @@ moe_status moe_kv_weights(moe_kv_ctx* ctx, const void* q, int64_t ldq, const flo
     a.decay = opt->decay;
     a.part = ctx->part;
     a.tickets = ctx->tickets;
-    return with_counters(ctx->tickets_clear, stream, [&](bool clear, hipStream_t s) { return launch_kv_weights(g.dtype, g.kv_format == MOE_KV_FP8, a, clear, s); });
+    return with_counters(ctx->tickets_clear, stream, [&](bool& clear, hipStream_t s) { return launch_kv_weights(g.dtype, g.kv_format == MOE_KV_FP8, a, clear, s); });
 }
 
 moe_status moe_kv_select(moe_kv_ctx* ctx, const float* scores, int64_t n_pages, const moe_kv_batch* batch, const moe_select_options* opt,

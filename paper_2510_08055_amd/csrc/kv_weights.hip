@@ -30,6 +30,8 @@ __device__ __forceinline__ int token_of(const WeightArgs& a, int r) { return a.G
 struct WeightSeq {
     int row0, n, p0, held;             // p0: the position of the first row; held: 0 where no score changes
     int lo;                            // the first token whose score changes
+    // pieces of tok tokens (a power of two), from multiples of it
+    __device__ __forceinline__ int units(int tok) const { return held > 0 ? (held - (lo & ~(tok - 1)) + tok - 1) / tok : 0; }
 };
 __device__ __forceinline__ WeightSeq seq_of(const WeightArgs& a, int s)
 {
@@ -91,8 +93,6 @@ template <typename T, bool FP8, int DP, int NJ> struct FewWeights {
     static constexpr int KC = DP / (F32 ? 16 : (FP8 ? 64 : 32));   // key loads per subtile
     static constexpr int KDIM = F32 ? 4 : (FP8 ? 16 : 8);          // dimensions of such a load
     static constexpr int KDW = KDIM * ESZ / 4;
-
-    static __device__ __forceinline__ int units(const WeightSeq& q) { return q.held > 0 ? (q.held - (q.lo & ~(TOK - 1)) + TOK - 1) / TOK : 0; }
 
     struct Queries {
         bf16x8_t b[F32 ? 1 : DP / 32];
@@ -354,6 +354,8 @@ template <typename T, bool FP8, int DP, bool EXACT> struct ManyWeights {
         int h, rows, tid, lane, n, half, wave, D;
         uint32_t lds0;
         float* lse;
+        bool even;                                       // rows of a load are of one token, or of whole tokens, and the stages begin with one
+        uint32_t lane_off, lane_chunk, lane_lse;         // then: where a lane's row and chunk are in a load, and its lse in a stage
 
         __device__ __forceinline__ Rows(const WeightArgs& a_, const WeightSeq& q_, int h_, char* smem) : a(a_), q(q_), h(h_)
         {
@@ -366,35 +368,51 @@ template <typename T, bool FP8, int DP, bool EXACT> struct ManyWeights {
             rows = q.n * a.G;
             lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_address(smem));
             lse = reinterpret_cast<float*>(smem + 2 * STAGE);
+            const int l = lane / CH;
+            even = (a.G % AT == 0 || AT % a.G == 0) && ROWS % a.G == 0;
+            lane_off = (uint32_t)(a.G % AT == 0 ? l * rowb() : token_of(a, l) * stride() + (l - token_of(a, l) * a.G) * rowb());
+            lane_chunk = (uint32_t)(((lane % CH) ^ swz(l)) * 16);
+            const int lr = wave * PER + lane, tok = token_of(a, lr);
+            lane_lse = (uint32_t)(tok * a.Hq + lr - tok * a.G) * 4;
         }
+        static constexpr int PER = ROWS / WAVES;         // rows of a wave's lse
+        __device__ __forceinline__ int rowb() const { return D * (int)sizeof(T); }
+        __device__ __forceinline__ int stride() const { return (int)a.ldq * (int)sizeof(T); }
 
         // Rows `first` on into a slot, straight into LDS, chunk c of row r to place c ^ swz(r).  A load has AT of them: where they are of one token, or of
         // whole tokens, only its address goes on from load to load; else, and where there are no more rows (the last one stands for them), every lane
         // finds its own.  (Rows of a load lie within 2^31 bytes: the launch sees to it.)
         __device__ __forceinline__ void fetch(int first, int slot) const
         {
-            const int stride = (int)a.ldq * (int)sizeof(T), rowb = D * (int)sizeof(T);
-            const bool all = (a.G % AT == 0 || AT % a.G == 0) && first + ROWS <= rows;
-            const uint32_t lane_off = (uint32_t)(a.G % AT == 0 ? lane / CH * rowb : lane / CH / a.G * stride + lane / CH % a.G * rowb);
-            auto aim = [&](int r, int tok0) {
-                const int rr = r < rows ? r : rows - 1, tok = token_of(a, rr);
-                return (uint32_t)((tok - tok0) * stride + (rr - tok * a.G) * rowb);
-            };
+            const T* const heads = static_cast<const T*>(a.q) + (int64_t)h * a.G * D;
+            const uint32_t lse_to = lds0 + 2 * STAGE + (slot * ROWS + wave * PER) * 4;
+            // (chunks past the dimension: no product reads them)
+            auto inside = [&](uint32_t chunk) { return EXACT || (int)chunk < rowb() ? chunk : 0; };
+            if (even && first + ROWS <= rows) {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int lr = (wave * LOADS + i) * AT, r = first + lr;
-                const int rr = r < rows ? r : rows - 1, tok = token_of(a, rr);
-                const int chunk = (lane % CH) ^ swz(lr + lane / CH);
-                const char* base = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (int64_t)(q.row0 + tok) * a.ldq + (int64_t)h * a.G * D);
-                // (chunks past the dimension: no product reads them)
-                const uint32_t off[1] = {(all ? lane_off : aim(r + lane / CH, tok)) + (chunk * 16 < rowb ? chunk * 16 : 0)};
-                load_lds_group(off, all ? base + (r - tok * a.G) * rowb : base, lds0 + slot * STAGE + lr * ROWB);
+                for (int i = 0; i < LOADS; ++i) {
+                    const int lr = (wave * LOADS + i) * AT, tok = token_of(a, first + lr);
+                    const char* base = reinterpret_cast<const char*>(heads + (int64_t)(q.row0 + tok) * a.ldq) + (first + lr - tok * a.G) * rowb();
+                    // (the bits of a load's row in lr and those of the lane's are others, and swz takes each to a place of its own)
+                    const uint32_t off[1] = {lane_off + inside(lane_chunk ^ (uint32_t)(swz(lr) * 16))};
+                    load_lds_group(off, base, lds0 + slot * STAGE + lr * ROWB);
+                }
+                if (lane < PER)
+                    load_lds_dword(lane_lse, reinterpret_cast<const char*>(a.lse + (int64_t)(q.row0 + token_of(a, first)) * a.Hq + h * a.G), lse_to);
+                return;
             }
-            constexpr int PER = ROWS / WAVES;        // rows of a wave's lse
+#pragma unroll 1
+            for (int i = 0; i < LOADS; ++i) {
+                const int lr = (wave * LOADS + i) * AT, r0 = first + lr < rows ? first + lr : rows - 1, tok0 = token_of(a, r0);
+                const int r = first + lr + lane / CH < rows ? first + lr + lane / CH : rows - 1, tok = token_of(a, r);
+                const char* base = reinterpret_cast<const char*>(heads + (int64_t)(q.row0 + tok0) * a.ldq);
+                const uint32_t off[1] = {(uint32_t)((tok - tok0) * stride() + (r - tok * a.G) * rowb()) + inside(lane_chunk ^ (uint32_t)(swz(lr) * 16))};
+                load_lds_group(off, base, lds0 + slot * STAGE + lr * ROWB);
+            }
             if (lane < PER) {
                 const int r = first + wave * PER + lane, rr = r < rows ? r : rows - 1, tok = token_of(a, rr), tok0 = token_of(a, first);
                 load_lds_dword((uint32_t)((tok - tok0) * a.Hq + rr - tok * a.G) * 4, reinterpret_cast<const char*>(a.lse + (int64_t)(q.row0 + tok0) * a.Hq + h * a.G),
-                               lds0 + 2 * STAGE + (slot * ROWS + wave * PER) * 4);
+                               lse_to);
             }
         }
 
@@ -489,6 +507,8 @@ template <typename T, bool FP8, int DP, bool EXACT> struct ManyWeights {
         Keys K;
         const int64_t row = place_of(a, q, seq, h, j0 + R.n);
         load_keys(a, row < 0 ? 0 : row, R.half, K);      // (a token that is not there: some row, its sum is not stored)
+        // (the compiler counts the loads it knows: waited for here, those of the keys are not waited for in the loop, where the next rows' are on the way)
+        __builtin_amdgcn_s_waitcnt(0x0f70);
         float acc[16] = {};
         int slot = 0;
         for (; r0 < r1; r0 += ROWS, slot ^= 1) {
@@ -520,7 +540,6 @@ template <typename T, bool FP8, int DP, bool EXACT> struct ManyWeights {
 
     // ---- sequences whose rows fit both slots: brought there once, they meet all tokens of a stretch; every wave for itself ----
     static __device__ __forceinline__ bool fit(const WeightArgs& a, const WeightSeq& q) { return (int64_t)q.n * a.G <= 2 * ROWS; }
-    static __device__ __forceinline__ int units(const WeightSeq& q) { return q.held > 0 ? (q.held - (q.lo & ~(WTOK - 1)) + WTOK - 1) / WTOK : 0; }
     // Tokens [begin, end) of a sequence and head, begin a multiple of 32.
     static __device__ __forceinline__ void run_held(const WeightArgs& a, const WeightSeq& q, int seq, int h, int begin, int end, char* smem)
     {
@@ -553,11 +572,11 @@ template <typename T, bool FP8, int DP, bool EXACT> struct ManyWeights {
     }
 };
 
+// Sums of a quantity over the sequences up to and with each, of kSeqs sequences.
 struct WeightPlan {
-    int64_t few[kSeqs], held[kSeqs], many[kSeqs];      // units and steps of the sequences up to and with each
-    int64_t sums[3][8];
+    int64_t upto[kSeqs];
+    int64_t sums[8];
 };
-
 __device__ __forceinline__ int64_t scan64(int64_t v)
 {
     for (int d = 1; d < 64; d *= 2) {
@@ -566,173 +585,166 @@ __device__ __forceinline__ int64_t scan64(int64_t v)
     }
     return v;
 }
-// The first sequence whose sum is above x.
-__device__ __forceinline__ int found_in(const int64_t* sums, int64_t x)
+// Every thread of the block calls it, the first kSeqs with their sequence's value; a barrier comes between two plans that share LDS.
+__device__ __forceinline__ void make_plan(WeightPlan& plan, int64_t v)
+{
+    const int wave = threadIdx.x >> 6;
+    v = scan64(v);
+    if (lane_id() == 63) plan.sums[wave] = v;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) v += plan.sums[w];
+    if (threadIdx.x < kSeqs) plan.upto[threadIdx.x] = v;
+    __syncthreads();
+}
+// The first sequence whose sum is above x, and the sum before it.
+__device__ __forceinline__ int found_in(const WeightPlan& plan, int64_t x, int64_t& before)
 {
     int lo = 0, hi = kSeqs - 1;
     while (lo < hi) {
         const int mid = (lo + hi) / 2;
-        if (sums[mid] > x) hi = mid;
+        if (plan.upto[mid] > x) hi = mid;
         else lo = mid + 1;
     }
-    return __builtin_amdgcn_readfirstlane(lo);
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    before = lo > 0 ? plan.upto[lo - 1] : 0;
+    return lo;
 }
 
-// LIGHT: all sequences are taken for ones of few rows.
-template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> struct WeightKernel {
-    static constexpr bool F32 = sizeof(T) == 4;
-    typedef FewWeights<T, FP8, DP, F32 || (!LIGHT && DP > 64) ? 1 : 2> Few;
-    typedef ManyWeights<T, FP8, DP, EXACT> Many;
-    static constexpr int THREADS = LIGHT ? 256 : 64 * Many::WAVES;
-    // (64 decode rows over up to 8192 tokens, us, light blocks of a unit as here / one more: bf16 dim 128 44 / 54, 256 80 / 119, fp32 30 / -; / one fewer: bf16 64 47 / 51 with two
-    // fewer, FP8 128 27 / 29)
-    static constexpr int BLOCKS = LIGHT ? (DP > 128 ? 1 : DP > 64 ? (FP8 ? (F32 ? 2 : 3) : 2) : F32 ? 3 : 4) : DP > 128 || (F32 && DP > 64) ? 1 : 2;      // of a unit
-    static constexpr size_t PLAN_AT = LIGHT ? 0 : (Many::LDS + 15) / 16 * 16, LDS = PLAN_AT + sizeof(WeightPlan);
-};
-template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT>
-__global__ __launch_bounds__((WeightKernel<T, FP8, DP, EXACT, LIGHT>::THREADS), (WeightKernel<T, FP8, DP, EXACT, LIGHT>::BLOCKS * WeightKernel<T, FP8, DP, EXACT, LIGHT>::THREADS / 256)) void weights_kernel(WeightArgs a)
+// The stretch [x, end) of a plan of units (of tok tokens of a sequence and head): f(sequence's number in the plan, its data, head, tokens begin .. end - 1).
+template <typename F> __device__ __forceinline__ void each_span(const WeightArgs& a, const WeightPlan& plan, int s0, int tok, int64_t x, int64_t end, F f)
 {
-    typedef WeightKernel<T, FP8, DP, EXACT, LIGHT> K;
-    typedef typename K::Few Few;
-    typedef typename K::Many Many;
-    extern __shared__ __attribute__((aligned(256))) char smem[];
-    WeightPlan& plan = *reinterpret_cast<WeightPlan*>(smem + K::PLAN_AT);
-    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int Hk = a.c.Hk;
+    while (x < end) {
+        int64_t base;
+        const int i = found_in(plan, x, base);
+        const WeightSeq q = seq_of(a, s0 + i);
+        const int units = q.units(tok), h = (int)((x - base) / units), from = (int)(x - base - (int64_t)h * units);
+        const int to = end - x < units - from ? from + (int)(end - x) : units;
+        const int begin = (q.lo & ~(tok - 1)) + from * tok, stop = begin + (to - from) * tok < q.held ? begin + (to - from) * tok : q.held;
+        f(s0 + i, q, h, begin, stop);
+        x += to - from;
+    }
+}
+
+// Sequences of up to a.few_rows packed rows.  Blocks of a unit: 64 decode rows over up to 8192 tokens, us, as here / one more: bf16 dim 128 44 / 54, 256 80 / 119;
+// one fewer: FP8 128 27 / 29, fp32 128 30 / 37, two fewer: bf16 64 47 / 51.
+template <typename T, bool FP8, int DP> struct FewKernel {
+    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr int BLOCKS = DP > 128 ? 1 : DP > 64 ? (FP8 ? (F32 ? 2 : 3) : 2) : F32 ? 3 : 4;
+};
+template <typename T, bool FP8, int DP> __global__ __launch_bounds__(256, (FewKernel<T, FP8, DP>::BLOCKS)) void few_weights_kernel(WeightArgs a)
+{
+    typedef FewWeights<T, FP8, DP, sizeof(T) == 4 ? 1 : 2> Few;
+    __shared__ WeightPlan plan;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     for (int s0 = 0; s0 < a.c.S; s0 += kSeqs) {
         const int s = s0 + threadIdx.x;
-        int64_t few = 0, held = 0, many = 0;
-        if (threadIdx.x < kSeqs && s < a.c.S) {
+        int64_t units = 0;
+        if (s < a.c.S) {
             const WeightSeq q = seq_of(a, s);
-            if (LIGHT || q.n * a.G <= kFewRows) {
-                few = (int64_t)Few::units(q) * Hk;
-            } else if constexpr (!LIGHT) {
-                if (Many::fit(a, q)) {
-                    held = (int64_t)Many::units(q) * Hk;
-                } else {
-                    const Steps st = Many::steps_of(a, q);
-                    many = Many::before(st, st.end) * Hk;
-                }
-            }
+            if (q.n * a.G <= a.few_rows) units = (int64_t)q.units(Few::TOK) * a.c.Hk;
         }
-        few = scan64(few);
-        if constexpr (!LIGHT) {
-            held = scan64(held);
-            many = scan64(many);
-        }
-        if (lane == 63) {
-            plan.sums[0][wave] = few;
-            plan.sums[1][wave] = held;
-            plan.sums[2][wave] = many;
-        }
-        __syncthreads();
-        for (int w = 0; w < wave; ++w) {
-            few += plan.sums[0][w];
-            held += plan.sums[1][w];
-            many += plan.sums[2][w];
-        }
-        if (threadIdx.x < kSeqs) {
-            plan.few[threadIdx.x] = few;
-            plan.held[threadIdx.x] = held;
-            plan.many[threadIdx.x] = many;
-        }
-        __syncthreads();
-        if constexpr (!LIGHT) {
-            const int chunk = s0 / kSeqs;
-            const bool split = chunk < a.split_chunks;                       // (where there are no more slots, a tile is its first step's owner's)
-            const int64_t all = plan.many[kSeqs - 1];
-            const int64_t most = (all + kMinSteps - 1) / kMinSteps;
-            const int64_t blocks = most < gridDim.x ? most : gridDim.x;      // that have a stretch
-            auto cut = [&](int64_t b) { return b * all / blocks; };
-            if ((int64_t)blockIdx.x < blocks) {
-                // the stretch that step x lies in
-                auto owner = [&](int64_t x) {
-                    int64_t b = x * blocks / all;
-                    while (cut(b + 1) <= x) ++b;
-                    return (int)b;
-                };
-                const int64_t start = cut(blockIdx.x), end = cut(blockIdx.x + 1);
-                int64_t x = start;
-                while (x < end) {
-                    const int i = found_in(plan.many, x);
-                    const int64_t base = i > 0 ? plan.many[i - 1] : 0;
-                    const WeightSeq q = seq_of(a, s0 + i);
-                    const Steps st = Many::steps_of(a, q);
-                    const int64_t of_head = Many::before(st, st.end);
-                    const int h = (int)((x - base) / of_head);
-                    const int64_t head_base = base + h * of_head, rem = x - head_base;
-                    int lo = st.first, hi = st.end - 1;                      // the last tile that starts at or before rem
-                    while (lo < hi) {
-                        const int mid = (lo + hi + 1) / 2;
-                        if (Many::before(st, mid) <= rem) lo = mid;
-                        else hi = mid - 1;
-                    }
-                    for (int tile = lo; tile < st.end && x < end; ++tile) {
-                        const int64_t t_begin = head_base + Many::before(st, tile), t_end = head_base + Many::before(st, tile + 1);
-                        const int64_t to = !split || t_end < end ? t_end : end;
-                        if (split || x == t_begin) {
-                            int first = (int)blockIdx.x, last = first;
-                            if (split && t_begin < start) first = owner(t_begin);
-                            if (split && t_end > end) last = owner(t_end - 1);
-                            Many::run(a, q, st, s0 + i, h, tile, (int)(x - t_begin), (int)(to - t_begin), (int)blockIdx.x - first, last - first + 1,
-                                      chunk * (int)gridDim.x + first, smem);
-                            __syncthreads();
-                        }
-                        x = to;
-                    }
-                }
-            }
-        }
-        // a sequence's and head's tokens from unit `from` to `to`
-        auto span = [](const WeightSeq& q, int tok, int from, int to, int& begin, int& end) {
-            begin = (q.lo & ~(tok - 1)) + from * tok;
-            end = begin + (to - from) * tok < q.held ? begin + (to - from) * tok : q.held;
-        };
-        if constexpr (!LIGHT) {
-            const int64_t all = plan.held[kSeqs - 1];
-            int64_t x = blockIdx.x * all / gridDim.x;
-            const int64_t end = (blockIdx.x + 1) * all / gridDim.x;
-            while (x < end) {
-                const int i = found_in(plan.held, x);
-                const int64_t base = i > 0 ? plan.held[i - 1] : 0;
-                const WeightSeq q = seq_of(a, s0 + i);
-                const int units = Many::units(q), h = (int)((x - base) / units), from = (int)(x - base - (int64_t)h * units);
-                const int to = end - x < units - from ? from + (int)(end - x) : units;
-                int begin, stop;
-                span(q, Many::WTOK, from, to, begin, stop);
-                Many::run_held(a, q, s0 + i, h, begin, stop, smem);
-                __syncthreads();
-                x += to - from;
-            }
-        }
-        const int64_t all = plan.few[kSeqs - 1], waves = (int64_t)gridDim.x * (K::THREADS / 64), me = (int64_t)blockIdx.x * (K::THREADS / 64) + wave;
-        int64_t x = me * all / waves;
-        const int64_t end = (me + 1) * all / waves;
-        while (x < end) {
-            const int i = found_in(plan.few, x);
-            const int64_t base = i > 0 ? plan.few[i - 1] : 0;
-            const WeightSeq q = seq_of(a, s0 + i);
-            const int units = Few::units(q), h = (int)((x - base) / units), from = (int)(x - base - (int64_t)h * units);
-            const int to = end - x < units - from ? from + (int)(end - x) : units;
-            int begin, stop;
-            span(q, Few::TOK, from, to, begin, stop);
-            Few::run(a, q, s0 + i, h, begin, stop);
-            x += to - from;
-        }
+        make_plan(plan, units);
+        const int64_t all = plan.upto[kSeqs - 1], waves = (int64_t)gridDim.x * 4, me = (int64_t)blockIdx.x * 4 + wave;
+        each_span(a, plan, s0, Few::TOK, me * all / waves, (me + 1) * all / waves,
+                  [&](int seq, const WeightSeq& q, int h, int begin, int end) { Few::run(a, q, seq, h, begin, end); });
         __syncthreads();
     }
 }
 
-template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> hipError_t launch(WeightArgs a, bool clear_tickets, hipStream_t s)
+// Sequences of more packed rows.
+template <typename T, bool FP8, int DP, bool EXACT> struct RowsKernel {
+    typedef ManyWeights<T, FP8, DP, EXACT> Many;
+    static constexpr int THREADS = 64 * Many::WAVES, BLOCKS = DP > 128 || (sizeof(T) == 4 && DP > 64) ? 1 : 2;      // of a unit
+    static constexpr size_t PLAN_AT = (Many::LDS + 15) / 16 * 16, LDS = PLAN_AT + 2 * sizeof(WeightPlan);
+};
+template <typename T, bool FP8, int DP, bool EXACT>
+__global__ __launch_bounds__((RowsKernel<T, FP8, DP, EXACT>::THREADS), (RowsKernel<T, FP8, DP, EXACT>::BLOCKS * 2)) void rows_weights_kernel(WeightArgs a)
 {
-    typedef WeightKernel<T, FP8, DP, EXACT, LIGHT> K;
-    int units = 0;
-    hipError_t e = compute_units(&units);
-    if (e != hipSuccess) return e;
-    a.g_magic = a.G > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G) : 0;
+    typedef RowsKernel<T, FP8, DP, EXACT> K;
+    typedef typename K::Many Many;
+    extern __shared__ __attribute__((aligned(256))) char smem[];
+    WeightPlan *const held = reinterpret_cast<WeightPlan*>(smem + K::PLAN_AT), *const many = held + 1;
+    for (int s0 = 0; s0 < a.c.S; s0 += kSeqs) {
+        const int s = s0 + threadIdx.x;
+        int64_t units = 0, steps = 0;
+        if (threadIdx.x < kSeqs && s < a.c.S) {
+            const WeightSeq q = seq_of(a, s);
+            if (q.n * a.G > a.few_rows) {
+                if (Many::fit(a, q)) {
+                    units = (int64_t)q.units(Many::WTOK) * a.c.Hk;
+                } else {
+                    const Steps st = Many::steps_of(a, q);
+                    steps = Many::before(st, st.end) * a.c.Hk;
+                }
+            }
+        }
+        make_plan(*held, units);
+        make_plan(*many, steps);
+        const int chunk = s0 / kSeqs;
+        const bool split = chunk < a.split_chunks;                       // (where there are no more slots, a tile is its first step's owner's)
+        int64_t all = many->upto[kSeqs - 1];
+        const int64_t most = (all + kMinSteps - 1) / kMinSteps;
+        const int64_t blocks = most < gridDim.x ? most : gridDim.x;      // that have a stretch
+        auto cut = [&](int64_t b) { return b * all / blocks; };
+        if ((int64_t)blockIdx.x < blocks) {
+            // the stretch that step x lies in
+            auto owner = [&](int64_t x) {
+                int64_t b = x * blocks / all;
+                while (cut(b + 1) <= x) ++b;
+                return (int)b;
+            };
+            const int64_t start = cut(blockIdx.x), end = cut(blockIdx.x + 1);
+            int64_t x = start;
+            while (x < end) {
+                int64_t base;
+                const int i = found_in(*many, x, base);
+                const WeightSeq q = seq_of(a, s0 + i);
+                const Steps st = Many::steps_of(a, q);
+                const int64_t of_head = Many::before(st, st.end);
+                const int h = (int)((x - base) / of_head);
+                const int64_t head_base = base + h * of_head, rem = x - head_base;
+                int lo = st.first, hi = st.end - 1;                      // the last tile that starts at or before rem
+                while (lo < hi) {
+                    const int mid = (lo + hi + 1) / 2;
+                    if (Many::before(st, mid) <= rem) lo = mid;
+                    else hi = mid - 1;
+                }
+                for (int tile = lo; tile < st.end && x < end; ++tile) {
+                    const int64_t t_begin = head_base + Many::before(st, tile), t_end = head_base + Many::before(st, tile + 1);
+                    const int64_t to = !split || t_end < end ? t_end : end;
+                    if (split || x == t_begin) {
+                        int first = (int)blockIdx.x, last = first;
+                        if (split && t_begin < start) first = owner(t_begin);
+                        if (split && t_end > end) last = owner(t_end - 1);
+                        Many::run(a, q, st, s0 + i, h, tile, (int)(x - t_begin), (int)(to - t_begin), (int)blockIdx.x - first, last - first + 1,
+                                  chunk * (int)gridDim.x + first, smem);
+                        __syncthreads();
+                    }
+                    x = to;
+                }
+            }
+        }
+        all = held->upto[kSeqs - 1];
+        each_span(a, *held, s0, Many::WTOK, blockIdx.x * all / gridDim.x, (blockIdx.x + 1) * all / gridDim.x,
+                  [&](int seq, const WeightSeq& q, int h, int begin, int end) {
+                      Many::run_held(a, q, seq, h, begin, end, smem);
+                      __syncthreads();
+                  });
+        __syncthreads();
+    }
+}
+
+template <typename T, bool FP8, int DP> hipError_t launch_few(const WeightArgs& a, int units, hipStream_t s)
+{
+    few_weights_kernel<T, FP8, DP><<<(unsigned)(units * FewKernel<T, FP8, DP>::BLOCKS), 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+template <typename T, bool FP8, int DP, bool EXACT> hipError_t launch_rows(WeightArgs a, int units, bool clear_tickets, hipStream_t s)
+{
+    typedef RowsKernel<T, FP8, DP, EXACT> K;
     static bool done[kMaxDevices];
-    const auto kern = weights_kernel<T, FP8, DP, EXACT, LIGHT>;
-    e = ensure_lds_limit(kern, K::LDS, done);
+    const auto kern = rows_weights_kernel<T, FP8, DP, EXACT>;
+    hipError_t e = ensure_lds_limit(kern, K::LDS, done);
     if (e != hipSuccess) return e;
     if (clear_tickets && (e = launch_fill_zero(a.tickets, kPartUnits, s)) != hipSuccess) return e;
     int grid = units * K::BLOCKS;
@@ -743,17 +755,27 @@ template <typename T, bool FP8, int DP, bool EXACT, bool LIGHT> hipError_t launc
     return hipGetLastError();
 }
 
-template <typename T, bool FP8, int DP> hipError_t launch_by_rows(const WeightArgs& a, bool clear, hipStream_t s)
+template <typename T, bool FP8, int DP> hipError_t launch_by_rows(WeightArgs a, bool& clear, hipStream_t s)
 {
-    // (the rule of the attention's launch: batches of decode or drafted rows alone)
+    int units = 0;
+    hipError_t e = compute_units(&units);
+    if (e != hipSuccess) return e;
+    a.g_magic = a.G > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G) : 0;
+    // How rows spread over the sequences only the device knows.  A batch of decode or drafted rows alone, by the rule of the attention's launch, is one of few
+    // rows throughout; any other takes two launches, one for its sequences of few rows, if it can have any, and one for the rest.
     constexpr int kMostRows = 384;
     const int64_t rows = a.c.T, seqs = a.c.S, most = rows < seqs ? rows : rows - seqs + 1;
-    const bool light = rows * a.G <= kFewRows * seqs && most * a.G <= kMostRows;
-    if (light) return launch<T, FP8, DP, false, true>(a, clear, s);
-    return a.c.D == DP ? launch<T, FP8, DP, true, false>(a, clear, s) : launch<T, FP8, DP, false, false>(a, clear, s);
+    if (rows * a.G <= kFewRows * seqs && most * a.G <= kMostRows) {
+        a.few_rows = 0x7fffffff;
+        clear = false;
+        return launch_few<T, FP8, DP>(a, units, s);
+    }
+    a.few_rows = kFewRows;
+    if (seqs > 1 && (e = launch_few<T, FP8, DP>(a, units, s)) != hipSuccess) return e;
+    return a.c.D == DP ? launch_rows<T, FP8, DP, true>(a, units, clear, s) : launch_rows<T, FP8, DP, false>(a, units, clear, s);
 }
 
-template <typename T, bool FP8> hipError_t launch_by_dim(const WeightArgs& a, bool clear, hipStream_t s)
+template <typename T, bool FP8> hipError_t launch_by_dim(const WeightArgs& a, bool& clear, hipStream_t s)
 {
     if (a.c.D <= 64) return launch_by_rows<T, FP8, 64>(a, clear, s);
     if (a.c.D <= 128) return launch_by_rows<T, FP8, 128>(a, clear, s);
@@ -762,7 +784,7 @@ template <typename T, bool FP8> hipError_t launch_by_dim(const WeightArgs& a, bo
 
 }  // namespace
 
-hipError_t launch_kv_weights(int dtype, bool fp8, const WeightArgs& a, bool clear, hipStream_t s)
+hipError_t launch_kv_weights(int dtype, bool fp8, const WeightArgs& a, bool& clear, hipStream_t s)
 {
     if (dtype == MOE_BF16) return fp8 ? launch_by_dim<bf16_t, true>(a, clear, s) : launch_by_dim<bf16_t, false>(a, clear, s);
     return fp8 ? launch_by_dim<float, true>(a, clear, s) : launch_by_dim<float, false>(a, clear, s);
