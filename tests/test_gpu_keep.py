@@ -86,6 +86,16 @@ def test_weights_of_a_draft_among_decode_rows(gpu_lib, dtype, fmt, dim):
     check_weights(gpu_lib, b, causal=False, decay=0.0)
 
 
+@pytest.mark.parametrize("dtype,fmt,dim", [(torch.bfloat16, "", 128), (torch.bfloat16, "fp8", 64), (torch.float32, "", 64), (torch.float32, "fp8", 256)])
+@pytest.mark.parametrize("decode", [1, 17, 18, 60])
+def test_weights_of_a_prompt_among_decode_rows(gpu_lib, decode, dtype, fmt, dim):
+    """On both sides of where sequences of few rows have a launch of their own (here 17 and 18), a prompt, a piece of one and an empty sequence among them."""
+    rows, kv = [1] * decode + [300, 0, 17], [29 * i % 400 + 1 for i in range(decode)] + [700, 5, 90]
+    b = Batch(rows, kv, 8, 2, dim, 16, dtype, fmt, seed=decode)
+    check_weights(gpu_lib, b)
+    check_weights(gpu_lib, b, causal=False, window=100, decay=0.0)
+
+
 def test_weights_where_nothing_is_seen(gpu_lib):
     """No tokens; fewer tokens than rows; pages given back; a table that ends early; rows whose lse is minus infinity."""
     b = Batch([2, 5, 1, 2, 3], [0, 2, 40, 100, 90], 4, 2, 64, 16, seed=11, dropped=((2, 0), (2, 1), (2, 2), (3, 5), (3, 6), (4, 2), (4, 3)))
@@ -280,16 +290,16 @@ def test_compact_of_accepted_paths(gpu_lib):
     keep = keep[:, 0].contiguous()
     keep[1], lens[1] = torch.arange(start[1], start[1] + 16), 16
     lens[2], lens[3] = 0, -5
-    for first in (torch.tensor(start, dtype=torch.int32),):
-        want = lens.clamp(min=0)
-        tensors = [b.k_pages, b.v_pages]
-        ok = ref.compact([bits(t).cpu() for t in tensors], kv, b.table, 16, keep, want, first)
-        ctx, pages, batch = b.context(gpu_lib)
-        lens[0] = 1000                                    # (no more than max_keep count)
-        ok[0], ok[1] = ref.compact([bits(t).cpu() for t in tensors], kv, b.table, 16, keep, torch.where(lens > 16, 16, want), first)
-        ctx.moe_kv_compact(pages, batch, keep.to(DEV), lens.to(DEV), first=first.to(DEV))
-        for got, o in zip(tensors, ok):
-            assert torch.equal(bits(got).cpu(), o)
+    first = torch.tensor(start, dtype=torch.int32)
+    want = lens.clamp(min=0)
+    tensors = [b.k_pages, b.v_pages]
+    ok = ref.compact([bits(t).cpu() for t in tensors], kv, b.table, 16, keep, want, first)
+    ctx, pages, batch = b.context(gpu_lib)
+    lens[0] = 1000                                    # (no more than max_keep count)
+    ok[0], ok[1] = ref.compact([bits(t).cpu() for t in tensors], kv, b.table, 16, keep, torch.where(lens > 16, 16, want), first)
+    ctx.moe_kv_compact(pages, batch, keep.to(DEV), lens.to(DEV), first=first.to(DEV))
+    for got, o in zip(tensors, ok):
+        assert torch.equal(bits(got).cpu(), o)
 
 
 def test_compact_stays_within_the_sequences(gpu_lib):
