@@ -480,6 +480,13 @@ class KVContext:
                              f"not {t.dtype} {tuple(t.shape)} on {t.device}")
         return t.data_ptr()
 
+    def _output(self, t, name, dtype, shape):
+        """The caller's tensor, or a new one, and its pointer."""
+        if t is not None:
+            return t, self._dense(t, name, dtype, shape)
+        t = torch.empty(shape, dtype=dtype, device=self.workspace.device)
+        return t, t.data_ptr()
+
     def _rows(self, t, name, T, heads):
         """Pointer and row stride of a [T, heads, dim] tensor."""
         if t.shape != (T, heads, self.dim) or t.dtype != self.dtype or t.device != self.workspace.device:
@@ -558,12 +565,9 @@ class KVContext:
         the row of its sequence that it follows, or -1.  Sequences of more than 64 * words rows are prompts."""
         self._packed_batch(batch)
         T = parents.shape[0]
-        if masks is None:
-            masks = torch.empty((T, words), dtype=torch.int64, device=self.device)
-        if positions is None:
-            positions = torch.empty((T,), dtype=torch.int32, device=self.device)
-        self._call("moe_tree_masks", self._dense(parents, "parents", torch.int32, (T,)), T, batch, _int32("words", words), _int32("window", window),
-                   self._dense(masks, "masks", torch.int64, (T, words)), self._dense(positions, "positions", torch.int32, (T,)))
+        masks, mp = self._output(masks, "masks", torch.int64, (T, _int32("words", words)))
+        positions, pp = self._output(positions, "positions", torch.int32, (T,))
+        self._call("moe_tree_masks", self._dense(parents, "parents", torch.int32, (T,)), T, batch, words, _int32("window", window), mp, pp)
         return masks, positions
 
     def moe_tree_attention(self, q, pages, batch, masks, positions=None, window=0, sinks=None, out=None, lse=None):
@@ -598,14 +602,11 @@ class KVContext:
         """The tokens to keep [n_seqs, kv_heads, budget] int32, ascending, -1 behind them, and how many [n_seqs]."""
         self._packed_batch(batch)
         shape = (batch.n_seqs, self.kv_heads, _int32("budget", budget))
-        if keep is None:
-            keep = torch.empty(shape, dtype=torch.int32, device=self.device)
-        if keep_lens is None:
-            keep_lens = torch.empty(shape[:1], dtype=torch.int32, device=self.device)
+        keep, kp = self._output(keep, "keep", torch.int32, shape)
+        keep_lens, lp = self._output(keep_lens, "keep_lens", torch.int32, shape[:1])
         n = scores.shape[0]
         opt = CSelectOptions(shape[2], _int32("first", first), _int32("recent", recent))
-        self._call("moe_kv_select", self._dense(scores, "scores", torch.float32, (n, self.kv_heads, self.page)), n, batch, opt,
-                   self._dense(keep, "keep", torch.int32, shape), self._dense(keep_lens, "keep_lens", torch.int32, shape[:1]))
+        self._call("moe_kv_select", self._dense(scores, "scores", torch.float32, (n, self.kv_heads, self.page)), n, batch, opt, kp, lp)
         return keep, keep_lens
 
     def moe_kv_compact(self, pages, batch, keep, keep_lens, first=None, scores=None):
