@@ -431,7 +431,8 @@ typedef struct {
  * for every token j that is there, of the sequences that bring rows; with decay 0 no earlier score is read (it may be anything).  lse [T, heads] fp32 is what moe_paged_attention (with the same
  * causal and window) left: the w_j of a row are then its softmax weights, less the sink's share.  A row whose lse is minus infinity saw nothing and
  * adds nothing.  Only the keys of the pages are read.  Scores, exponentials and sums are fp32, in an order that depends on the batch alone: the same call
- * gives the same bits.  ldq is at most 2^23.  Rows may be the last ones of a prompt whose other rows are cached already, so that those alone are its judges.
+ * gives the same bits.  Of a page that several sequences of a batch share, or a sequence's table has twice, the scores are unspecified: it has no one
+ * history to be judged in.  ldq is at most 2^23.  Rows may be the last ones of a prompt whose other rows are cached already, so that those alone are its judges.
  */
 moe_status moe_kv_weights(moe_kv_ctx *ctx, const void *q, int64_t ldq, const float *lse, int64_t T, const moe_kv_pages *pages,
                           const moe_kv_batch *batch, const moe_weights_options *opt, float *scores, void *stream);

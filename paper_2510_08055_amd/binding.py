@@ -589,7 +589,8 @@ class KVContext:
         return out
 
     def moe_kv_weights(self, q, lse, pages, batch, scores, causal=True, window=0, decay=1.0):
-        """Adds the attention weights of the rows to scores [n_pages, kv_heads, page] fp32, in place; lse as moe_paged_attention left it."""
+        """Adds the attention weights of the rows to scores [n_pages, kv_heads, page] fp32, in place; lse as moe_paged_attention left it.
+        Pages that sequences share have unspecified scores."""
         self._packed(pages, batch)
         T = q.shape[0]
         qp, ldq = self._rows(q, "q", T, self.heads)

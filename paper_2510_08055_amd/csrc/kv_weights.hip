@@ -2,16 +2,17 @@
 //
 // Scores are computed transposed as in the attention, S = K Q^T, a query row to a lane's column: a row's lse is lane-local, and the sums of the
 // exponentials over the rows stay in the lanes until the end.  There are three ways to bring rows and keys together, by the packed rows of a sequence:
-//   up to 16: the rows stay in registers, and the keys stream by, read once, which bounds it.  64 rows over up to 8192 tokens, 188 MB of keys, 43.5 us,
-//     4.4 TB/s (a copy of 4 GiB 4.8).  Keys are plain loads: an instruction takes half a line of each row (as a stream 54 -> 57 us).
+//   up to 16: the rows stay in registers, and the keys stream by, read once, which bounds it.  64 rows over up to 8192 tokens, 188 MB of keys, 44 us,
+//     4.3 TB/s (a copy of 4 GiB 4.8).  Keys are plain loads: an instruction takes half a line of each row (as a stream 54 -> 57 us).
 //   up to what LDS holds (256; fp32 128): the rows stay there, and every wave takes 32 tokens' keys for itself, with no barrier until the end.
 //     What bounds it: VALU, and the chain page table, keys, products of each 32 tokens.  32 rows of 64 heads over up to 16384 FP8 tokens in 12 sequences
-//     46 us (61 as more rows are taken).
+//     44 us (61 as more rows are taken).  Sequences of fewer rows beside such, or beside prompts, are taken this way too.
 //   more: a block holds 256 tokens' keys, 32 to a wave, and takes the rows that see them 128 at a time from LDS, brought there by direct
-//     loads while the 128 before are used.  What bounds it: a prompt of 8192 rows and 32 heads, dim 128, takes 350 us (0.79 PFLOP/s); VALU busy 54 % and the matrix pipes
-//     32 % of them, with four waves to a SIMD; waves wait 44 % of their cycles, most of that for products that follow each other and for LDS (300 us with no rows brought).
+//     loads while the 128 before are used.  What bounds it: a prompt of 8192 rows and 32 heads, dim 128, takes 350 us (0.79 PFLOP/s); VALU busy 51 % and the matrix pipes
+//     34 % of them, with four waves to a SIMD; waves wait 44 % of their cycles, most of that for products that follow each other and for LDS (300 us with no rows brought).
 //     Fewer waves with more each were slower: 64 tokens to a wave 440 to 500 us, and with the products of one half of them beside the exponentials of the other,
-//     scheduled by hand, 445 (two waves to a SIMD) and 610 (one); stages of 64 rows, four in flight, 380; neighbouring stretches on one XCD 367.
+//     scheduled by hand, 445 (two waves to a SIMD) and 610 (one); stages of 64 rows, four in flight, 380; neighbouring stretches on one XCD 367;
+//     reads of LDS two, four or eight products ahead 349, 384 and 428 (128 registers do not hold them).
 //
 // Work is cut on the device, from the descriptors, into equal stretches: of units of 16 or 32 tokens of all sequences and heads, a stretch to a wave or a
 // block; of steps (128 packed rows by 256 tokens) where rows are many, a stretch to a block.  A token's sum belongs to one wave, or is joined from the
