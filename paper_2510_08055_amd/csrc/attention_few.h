@@ -373,7 +373,8 @@ template <typename T, bool FP8, int DP, int NQ, bool EXACT, bool TREE> struct Fe
     }
 
     // The weights as the second product's operand.  bf16: rounded to nearest, 2^-8 of a weight at most; the sum they are divided by is that
-    // of the unrounded ones, in fp32.  (A split into two bf16 halves would double the product for an output that is rounded to bf16 anyway.)
+    // of the unrounded ones, in fp32.  (A split into two bf16 halves would double the product for an output that is rounded to bf16 anyway: measured
+    // on trees, an output's relative error falls from 0.0023 to the 0.0017 of its own rounding, 26 rows over 700 tokens 21.0 -> 22.4 us, 32 trees 135 -> 158.)
     struct Weights {
         bf16x8_t b[F32 ? 1 : NQ];
         float f[F32 ? NQ : 1][4];
