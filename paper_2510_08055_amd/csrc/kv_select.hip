@@ -205,14 +205,15 @@ template <int N> __device__ __forceinline__ void list_tokens(const SelectArgs& a
 
 template <int N> __device__ __forceinline__ void read_keys(const SelectArgs& a, const Sequence& q, int j0, Four (&f)[N])
 {
-    constexpr int AT_ONCE = N < 8 ? N : 8;
+    constexpr int AT_ONCE = N < 8 ? N : 8;      // (12 are eight and four)
 #pragma unroll
     for (int i0 = 0; i0 < N; i0 += AT_ONCE) {
+        const int n = N - i0 < AT_ONCE ? N - i0 : AT_ONCE;
         int id[AT_ONCE];
 #pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i) id[i] = page_id(a, q, j0 + (i0 + i) * 4 * kThreads + (int)threadIdx.x * 4);
+        for (int i = 0; i < n; ++i) id[i] = page_id(a, q, j0 + (i0 + i) * 4 * kThreads + (int)threadIdx.x * 4);
 #pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i) f[i0 + i] = keys_of(a, q, j0 + (i0 + i) * 4 * kThreads + (int)threadIdx.x * 4, id[i]);
+        for (int i = 0; i < n; ++i) f[i0 + i] = keys_of(a, q, j0 + (i0 + i) * 4 * kThreads + (int)threadIdx.x * 4, id[i]);
         if (i0 + AT_ONCE < N) __builtin_amdgcn_sched_barrier(0);
     }
 }
