@@ -38,3 +38,19 @@ def test_select_of_many_long_sequences(gpu_lib, scores, budget, first, recent):
     elif scores == "two values":
         x = (x > 0.5).float()
     check_select(gpu_lib, x, kv, table, page, budget, first, recent)
+
+
+@pytest.mark.parametrize("budget,first,recent", [(1, 0, 0), (5000, 4, 256), (60000, 0, 0)])
+def test_select_of_tables_that_the_workspace_does_not_hold(gpu_lib, budget, first, recent):
+    """Few sequences in parts need words for every token that a table could name; where there are too few, a block has each sequence to itself."""
+    page, hk = 256, 2
+    kv = [70000, 5, 16385, 49152, 0]
+    x, table, _ = lists(kv, page, hk, seed=budget, dropped=[(0, 3), (0, 200), (2, 0)])
+    wide = torch.full((len(kv), 2 ** 20 // page), -1, dtype=torch.int32, device=DEV)
+    wide[:, :table.shape[1]] = table
+    assert len(kv) * hk < units() and len(kv) * hk * 2 ** 20 * 4 > gpu_lib.kv_workspace_bytes(hk, hk, 32, page, torch.float32)
+    check_select(gpu_lib, x, kv, wide, page, budget, first, recent)
+    kv[4] = 2 ** 20 + 77                                  # past the table; of all that only its last page is there
+    wide[4, -1] = int((~torch.isin(torch.arange(x.shape[0], device=DEV), wide.long())).nonzero()[0])
+    check_select(gpu_lib, x, kv, wide, page, budget, first, recent)
+
