@@ -109,12 +109,10 @@ def _early_uses_of_async_loads(asm, kernel):
     return bad
 
 
-def _early_uses_on_any_path(asm, kernel):
-    """Instructions that name the destination of an asm-issued global_load_dword before the next vmcnt wait, in every
-    function whose (mangled) name contains `kernel`; every path from the load is followed, branches included (for kernels without
-    waits that only a repeated test of the same condition pairs with their loads)."""
+def _listings(asm, kernel):
+    """The functions whose (mangled) name contains `kernel`: name, instructions as (text, issued from inline asm), places of the labels."""
     import re
-    bad, funcs, cur = [], [], None
+    funcs, cur = [], None
     for line in asm.splitlines():
         m = re.match(r"^(_Z\S+):", line)
         if m:
@@ -125,7 +123,7 @@ def _early_uses_on_any_path(asm, kernel):
         if cur is not None:
             cur.append(line)
     for name, lines in funcs:
-        code, labels, in_asm = [], {}, False      # (text, issued from inline asm)
+        code, labels, in_asm = [], {}, False
         for line in lines:
             m = re.match(r"^(\.?\w+):", line)
             if m:
@@ -137,6 +135,16 @@ def _early_uses_on_any_path(asm, kernel):
             text = line.split(";")[0].strip()
             if text and not text.startswith("."):
                 code.append((text, in_asm))
+        yield name, code, labels
+
+
+def _early_uses_on_any_path(asm, kernel):
+    """Instructions that name the destination of an asm-issued global_load_dword before the next vmcnt wait, in every
+    function whose (mangled) name contains `kernel`; every path from the load is followed, branches included (for kernels without
+    waits that only a repeated test of the same condition pairs with their loads)."""
+    import re
+    bad = []
+    for name, code, labels in _listings(asm, kernel):
         named = []
         for text, _ in code:
             regs = set(int(r) for r in re.findall(r"\bv(\d+)\b", text))
@@ -167,10 +175,45 @@ def _early_uses_on_any_path(asm, kernel):
     return bad
 
 
+# Kernels of these files mark what they have done with stores that other blocks poll, and count themselves as ended with an atomic; the block that
+# ends last clears the marks.  A store and a later atomic to another address may arrive in either order, so a mark has to be waited for before the count: else it could
+# land on the cleared word, and the next launch would find it.
+MARKS_BEFORE_COUNTS = {"kv_compact.hip": "compact_tiles_kernel"}
+
+
+def _marks_behind_counts(asm, kernel):
+    """Atomics that a path reaches from a store to the level all blocks see (sc1) without a wait for it (vmcnt(0)), in every function whose (mangled) name contains
+    `kernel`."""
+    import re
+    bad = []
+    for name, code, labels in _listings(asm, kernel):
+        todo = [i + 1 for i, (t, _) in enumerate(code) if re.match(r"global_store_\w+ .*\bsc1\b", t)]
+        if not todo:
+            bad.append(f"{name[:60]}...: no store of a mark was found")
+        seen = set()
+        while todo:
+            i = todo.pop()
+            if i in seen or i >= len(code):
+                continue
+            seen.add(i)
+            t = code[i][0]
+            if re.match(r"s_waitcnt .*vmcnt\(0\)", t) or t.startswith("s_endpgm"):
+                continue
+            if t.startswith("global_atomic_"):
+                bad.append(f"{name[:60]}...: {t}")
+                continue
+            m = re.match(r"s_c?branch\w*\s+(\.?\w+)", t)
+            if m:
+                todo.append(labels[m.group(1)])
+            if not t.startswith("s_branch"):
+                todo.append(i + 1)
+    return bad
+
+
 def _compile(src, verbose):
     out = os.path.join(OBJ, src.replace(".hip", ".o"))
     extra = ["-Rpass-analysis=kernel-resource-usage"] if src in NO_SCRATCH else []
-    if src in M0_ONLY_FOR_LDS_LOADS:
+    if src in M0_ONLY_FOR_LDS_LOADS or src in MARKS_BEFORE_COUNTS:
         extra.append("-save-temps=obj")
     cmd = ["hipcc", *FLAGS, *extra, "-c", os.path.join(CSRC, src), "-o", out]
     if verbose:
@@ -198,6 +241,11 @@ def _compile(src, verbose):
             if bad:
                 raise RuntimeError(f"{src}: an asynchronously loaded register is used before its wait:\n  "
                                    + "\n  ".join(bad[:10]))
+    if src in MARKS_BEFORE_COUNTS:
+        with open(os.path.join(OBJ, src.replace(".hip", "-hip-amdgcn-amd-amdhsa-gfx950.s"))) as f:
+            bad = _marks_behind_counts(f.read(), MARKS_BEFORE_COUNTS[src])
+        if bad:
+            raise RuntimeError(f"{src}: blocks count themselves as ended before their marks have arrived:\n  " + "\n  ".join(bad[:10]))
     # the host pass does not know the GPU-only target feature (that warning is expected); the resource
     # remarks are only read by the check above
     log = "\n".join(l for l in r.stdout.splitlines()

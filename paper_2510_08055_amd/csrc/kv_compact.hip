@@ -107,8 +107,8 @@ template <int L, int U> struct Tile {
 
 __device__ __forceinline__ int64_t count_of(const CompactArgs& a, int s) { return a.lens[s] < a.max_keep ? a.lens[s] : a.max_keep; }
 
-// Every thread's loads have arrived (what they read may be overwritten).
-__device__ __forceinline__ void have_read()
+// Every thread's loads have arrived (what they read may be overwritten), and its stores.
+__device__ __forceinline__ void all_arrived()
 {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -123,13 +123,15 @@ template <int L, int U> __global__ __launch_bounds__(256) void compact_kernel(Co
         Tile<L, U> t;
         if (!__syncthreads_or(t.find(a, s, h, i, count))) continue;
         t.read(a, row);
-        have_read();
+        all_arrived();
         t.write(a, row);
     }
 }
 
 // A block to a tile.  state, of each sequence and head: the next tile to draw, the blocks that have ended, then a word for every tile that has
-// been read; zero between launches: the block that ends last leaves it so.  (One pair of counters for all blocks cost 16 histories 60 us of waiting for them.)
+// been read; zero between launches: the block that ends last leaves it so.  A block counts itself as ended once its mark has arrived, so that no mark lands on a word
+// that is cleared already (stores and atomics to different words keep no order of their own).  (One pair of counters for all blocks cost 16 histories 60 us of
+// waiting for them.)
 template <int L, int U> __global__ __launch_bounds__(256) void compact_tiles_kernel(CompactArgs a, int row, int items, int tiles, uint32_t* state)
 {
     __shared__ uint32_t drawn;
@@ -145,7 +147,7 @@ template <int L, int U> __global__ __launch_bounds__(256) void compact_tiles_ker
         Tile<L, U> t;
         const bool moves = __syncthreads_or(t.find(a, s, h, i0, count)) != 0;
         if (moves) t.read(a, row);
-        have_read();
+        all_arrived();
         if (threadIdx.x == 0) store_shared(read + tile, 1u);
         if (moves) {
             for (int i = threadIdx.x; i < tile; i += 256)
@@ -154,7 +156,7 @@ template <int L, int U> __global__ __launch_bounds__(256) void compact_tiles_ker
             t.write(a, row);
         }
     }
-    __syncthreads();
+    all_arrived();
     if (threadIdx.x == 0) drawn = __hip_atomic_fetch_add(mine + 1, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
     if (drawn != (uint32_t)tiles - 1) return;

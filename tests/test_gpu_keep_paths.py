@@ -3,7 +3,8 @@ import pytest
 import torch
 
 import keep_reference as ref
-from test_gpu_keep import lists
+from kv_reference import Batch
+from test_gpu_keep import bits, graphed, lists, random_keep, scores_of
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -54,3 +55,78 @@ def test_select_of_tables_that_the_workspace_does_not_hold(gpu_lib, budget, firs
     wide[4, -1] = int((~torch.isin(torch.arange(x.shape[0], device=DEV), wide.long())).nonzero()[0])
     check_select(gpu_lib, x, kv, wide, page, budget, first, recent)
 
+
+
+def words(max_keep, items, dim, dtype):
+    """Tiles of a list, and the words that all of them take (a word to a tile and two counters; 65536 are there)."""
+    lanes = next(n for n in (4, 8, 16, 32, 64) if n >= dim * torch.empty(0, dtype=dtype).element_size() // 16)
+    tiles = -(-max_keep // (256 // lanes * 8))
+    return tiles, items * (tiles + 2)
+
+
+def moved(b, keep, lens, scores):
+    """What a compaction leaves, as bytes."""
+    return ref.compact([bits(t).cpu() for t in (b.k_pages, b.v_pages, scores)], b.kv, b.table, b.page, keep, lens, None)
+
+
+def assert_moved(b, scores, want):
+    for got, ok in zip((b.k_pages, b.v_pages, scores), want):
+        assert torch.equal(bits(got).cpu(), ok)
+
+
+LAYOUTS = [([1000, 700, 900], 600, True), ([400] * 7, 300, False), ([5000], 4900, True), ([0, 3, 1500], 1400, True), ([1000, 700, 900], 600, True),
+           ([260] * 40, 257, True), ([3000, 2000], 129, False), ([5000], 4900, True)]
+
+
+def layout(kv, budget, per_head, seed):
+    b = Batch([0] * len(kv), kv, 2, 2, 128, 16, seed=seed)
+    keep, lens = random_keep(kv, 2, budget, seed)
+    if not per_head:
+        keep = keep[:, 0].contiguous()
+    tiles, n = words(budget, 2 * len(kv), 128, torch.bfloat16)
+    assert tiles > 1 and n <= 65536
+    return b, keep, lens, scores_of(b)
+
+
+def test_compact_again_and_again(gpu_lib):
+    """Lists of several tiles by one context, in layouts that put counters where others had marks: every call finds what the one before left."""
+    made = [layout(*how, seed=i) for i, how in enumerate(LAYOUTS)]
+    want = [moved(*x) for x in made]
+    ctx = made[0][0].context(gpu_lib)[0]
+    for b, keep, lens, scores in made:
+        ctx.moe_kv_compact(ctx.pack_pages(*b.pages()), ctx.pack_batch(b.row_offsets, b.kv_lens, b.table), keep.to(DEV), lens.to(DEV), scores=scores)
+    for (b, _, _, scores), w in zip(made, want):
+        assert_moved(b, scores, w)
+
+
+@pytest.mark.parametrize("warm", [False, True])
+def test_captured_compaction_of_tiles_replays(gpu_lib, warm):
+    """A graph of lists of several tiles, replayed over new lists, with eager calls of other layouts between."""
+    b, keep, lens, scores = layout([1000, 700, 900], 600, True, 3)
+    other, other_keep, other_lens, other_scores = layout([400] * 7, 300, False, 4)
+    ctx, pages, batch = b.context(gpu_lib)
+    lists_of, lens_of = torch.empty_like(keep, device=DEV), torch.empty_like(lens, device=DEV)
+    start = [t.clone() for t in (b.k_pages, b.v_pages, scores, other.k_pages, other.v_pages, other_scores)]
+    held = (b.k_pages, b.v_pages, scores, other.k_pages, other.v_pages, other_scores)
+
+    def eager():
+        ctx.moe_kv_compact(ctx.pack_pages(*other.pages()), ctx.pack_batch(other.row_offsets, other.kv_lens, other.table), other_keep.to(DEV),
+                           other_lens.to(DEV), scores=other_scores)
+
+    other_want = moved(other, other_keep, other_lens, other_scores)
+    if warm:
+        eager()
+        torch.cuda.synchronize()
+    replay = graphed(lambda: ctx.moe_kv_compact(pages, batch, lists_of, lens_of, scores=scores))
+    for i in range(4):
+        for t, w in zip(held, start):
+            t.copy_(w)
+        keep, lens = random_keep(b.kv, 2, 600, 50 + i)
+        lists_of.copy_(keep)
+        lens_of.copy_(lens)
+        want = moved(b, keep, lens, scores)
+        replay()
+        if i % 2:
+            eager()
+            assert_moved(other, other_scores, other_want)
+        assert_moved(b, scores, want)
