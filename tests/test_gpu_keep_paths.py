@@ -130,3 +130,26 @@ def test_captured_compaction_of_tiles_replays(gpu_lib, warm):
             eager()
             assert_moved(other, other_scores, other_want)
         assert_moved(b, scores, want)
+
+
+@pytest.mark.parametrize("dim,dtype,budget,seqs", [(128, torch.bfloat16, 1000, 1700), (256, torch.float32, 200, 1850), (16, torch.bfloat16, 2000, 2750)])
+def test_compact_of_more_lists_than_there_are_words(gpu_lib, dim, dtype, budget, seqs):
+    """Lists whose tiles outnumber the counters: a block takes a sequence and head, tile after tile.  Then by the same context few that do not."""
+    hk = 4
+    tiles, n = words(budget, seqs * hk, dim, dtype)
+    assert tiles > 3 and n > 65536
+    long = {0: 3 * budget, 7: budget + 1, 700: budget, seqs - 1: budget + budget // 2}
+    kv = [long.get(s, s % 5) for s in range(seqs)]
+    b = Batch([0] * seqs, kv, hk, hk, dim, 16, dtype, seed=dim)
+    keep, lens = random_keep(kv, hk, budget, 2)
+    scores = scores_of(b)
+    want = moved(b, keep, lens, scores)
+    ctx, pages, batch = b.context(gpu_lib)
+    ctx.moe_kv_compact(pages, batch, keep.to(DEV), lens.to(DEV), scores=scores)
+    assert_moved(b, scores, want)
+    few = Batch([0], [3 * budget], hk, hk, dim, 16, dtype, seed=1)
+    keep, lens = random_keep(few.kv, hk, budget, 3)
+    scores = scores_of(few)
+    want = moved(few, keep, lens, scores)
+    ctx.moe_kv_compact(ctx.pack_pages(*few.pages()), ctx.pack_batch(few.row_offsets, few.kv_lens, few.table), keep.to(DEV), lens.to(DEV), scores=scores)
+    assert_moved(few, scores, want)
