@@ -433,6 +433,10 @@ typedef struct {
  * adds nothing.  Only the keys of the pages are read.  Scores, exponentials and sums are fp32, in an order that depends on the batch alone: the same call
  * gives the same bits.  Of a page that several sequences of a batch share, or a sequence's table has twice, the scores are unspecified: it has no one
  * history to be judged in.  ldq is at most 2^23.  Rows may be the last ones of a prompt whose other rows are cached already, so that those alone are its judges.
+ * The call takes no masks: a sequence's new rows are a chain to it.  The rows of a tree must not be passed as they are (their siblings and what hangs from them would
+ * receive weight that no row gave them, and a window would count slots, not positions), nor can the call tell that they are a tree's.  Once a draft is verified and
+ * moe_kv_compact has moved its accepted path up, that path is a chain: a batch of the accepted rows alone, in their order, with the new lengths, their queries and the lse that
+ * moe_tree_attention gave them (with the same window) is what moe_kv_weights takes.
  */
 moe_status moe_kv_weights(moe_kv_ctx *ctx, const void *q, int64_t ldq, const float *lse, int64_t T, const moe_kv_pages *pages,
                           const moe_kv_batch *batch, const moe_weights_options *opt, float *scores, void *stream);

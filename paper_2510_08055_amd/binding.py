@@ -590,7 +590,8 @@ class KVContext:
 
     def moe_kv_weights(self, q, lse, pages, batch, scores, causal=True, window=0, decay=1.0):
         """Adds the attention weights of the rows to scores [n_pages, kv_heads, page] fp32, in place; lse as moe_paged_attention left it.
-        Pages that sequences share have unspecified scores."""
+        Pages that sequences share have unspecified scores.  Rows are chains: of a tree only the accepted ones can be passed, after moe_kv_compact, with
+        the new lengths and the lse that moe_tree_attention gave them."""
         self._packed(pages, batch)
         T = q.shape[0]
         qp, ldq = self._rows(q, "q", T, self.heads)
