@@ -8,7 +8,7 @@
 //     What bounds it: VALU, and the chain page table, keys, products of each 32 tokens.  32 rows of 64 heads over up to 16384 FP8 tokens in 12 sequences
 //     44 us (61 as more rows are taken).  Sequences of fewer rows beside such, or beside prompts, are taken this way too.
 //   more: a block holds 256 tokens' keys, 32 to a wave, and takes the rows that see them 128 at a time from LDS, brought there by direct
-//     loads while the 128 before are used.  What bounds it: a prompt of 8192 rows and 32 heads, dim 128, takes 350 us (0.79 PFLOP/s); VALU busy 51 % and the matrix pipes
+//     loads while the 128 before are used.  What bounds it: a prompt of 8192 rows and 32 heads, dim 128, takes 344 to 350 us by card (0.8 PFLOP/s); VALU busy 51 % and the matrix pipes
 //     34 % of them, with four waves to a SIMD; waves wait 44 % of their cycles, most of that for products that follow each other and for LDS (300 us with no rows brought).
 //     Fewer waves with more each were slower: 64 tokens to a wave 440 to 500 us, and with the products of one half of them beside the exponentials of the other,
 //     scheduled by hand, 445 (two waves to a SIMD) and 610 (one); stages of 64 rows, four in flight, 380; neighbouring stretches on one XCD 367;
@@ -652,7 +652,9 @@ template <typename T, bool FP8, int DP> __global__ __launch_bounds__(256, (FewKe
     }
 }
 
-// Sequences of more packed rows than a.few_rows.
+// Sequences of more packed rows than a.few_rows.  Registers kept in scratch: 7 at 128 dimensions in bf16 (FP8 pages 8), 21 at 80 to 112; fp32 16 below 64 and 81
+// (FP8 pages 54) at 144 to 240.  A prompt of 2048 rows, 32 heads over 4, bf16, us: 48 dimensions 43, 64 42, 80 51, 96 52, 112 53, 128 49, 144 60, 208 66, 256 68 (FP8 the
+// same within 2 %); fp32, 1024 rows: 54, 55, 53, 59, 63, 63, 78, 99, 106.
 template <typename T, bool FP8, int DP, bool EXACT> struct RowsKernel {
     typedef ManyWeights<T, FP8, DP, EXACT> Many;
     static constexpr int THREADS = 64 * Many::WAVES, BLOCKS = DP > 128 || (sizeof(T) == 4 && DP > 64) ? 1 : 2;      // of a unit
@@ -764,8 +766,12 @@ template <typename T, bool FP8, int DP> hipError_t launch_by_rows(WeightArgs a, 
     a.g_magic = a.G > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G) : 0;
     // How rows spread over the sequences only the device knows.  A batch of decode or drafted rows alone, by the rule of the attention's launch, is one of few
     // rows throughout; one that is mostly such takes two launches, one for its sequences of few rows and one for the rest; in any other the kernel of many rows
-    // takes all.  A prompt's 512 rows among decode rows, heads 32 / 4, us, one launch / two: 31 decode rows bf16 75 / 82; 63 FP8 83 / 84; 95 bf16 100 / 106,
-    // FP8 96 / 90; 255 bf16 162 / 166, FP8 143 / 125.
+    // takes all.  A prompt's 512 rows over 8192 tokens among decode rows, dim 128, us, one launch / two, decode rows over up to 4096 tokens and, in brackets, 300:
+    //   groups of 8, 4 key/value heads: 31 rows bf16 75 / 82; 63 FP8 83 / 84; behind the line 95 bf16 99 / 106 (70 / 72), FP8 94 / 90 (70 / 73), fp32 392 / 376;
+    //     255 bf16 160 / 166 (82 / 77), FP8 143 / 125 (83 / 76), fp32 528 / 488
+    //   groups of 4, 8 heads: 40 bf16 90 / 96 (68 / 66), FP8 87 / 81 (67 / 66), fp32 386 / 373; 255 bf16 262 / 255 (106 / 79), FP8 221 / 174 (110 / 75), fp32 762 / 670
+    //   groups of one, 8 heads: 10 bf16 37 / 41 (31 / 33), FP8 39 / 39 (32 / 35), fp32 117 / 116; 255 bf16 235 / 223 (74 / 46), FP8 192 / 144 (79 / 44), fp32 547 / 452
+    // (What two launches lose near the line, in bf16 above all, is a few us; what they save behind it grows with the decode rows, the more the fewer heads a group has.)
     constexpr int kMostRows = 384;
     const int64_t rows = a.c.T, seqs = a.c.S, most = rows < seqs ? rows : rows - seqs + 1;
     if (rows * a.G <= kFewRows * seqs && most * a.G <= kMostRows) {
