@@ -430,8 +430,8 @@ typedef struct {
  *   score_j = w_j for the tokens of the new rows themselves, decay * score_j + w_j for those before them
  * for every token j that is there, of the sequences that bring rows; with decay 0 no earlier score is read (it may be anything).  lse [T, heads] fp32 is what moe_paged_attention (with the same
  * causal and window) left: the w_j of a row are then its softmax weights, less the sink's share.  A row whose lse is minus infinity saw nothing and
- * adds nothing.  Only the keys of the pages are read.  Scores, exponentials and sums are fp32, in an order that depends on the batch alone: the same call
- * gives the same bits.  Of a page that several sequences of a batch share, or a sequence's table has twice, the scores are unspecified: it has no one
+ * adds nothing.  Only the keys of the pages are read (a layer's pages are handed over whole all the same: NULL values or scales are refused as
+ * in the other calls).  Scores, exponentials and sums are fp32, in an order that depends on the batch alone: the same call gives the same bits.  Of a page that several sequences of a batch share, or a sequence's table has twice, the scores are unspecified: it has no one
  * history to be judged in.  ldq is at most 2^23.  Rows may be the last ones of a prompt whose other rows are cached already, so that those alone are its judges.
  * The call takes no masks: a sequence's new rows are a chain to it.  The rows of a tree must not be passed as they are (their siblings and what hangs from them would
  * receive weight that no row gave them, and a window would count slots, not positions), nor can the call tell that they are a tree's.  Once a draft is verified and

@@ -4,7 +4,8 @@
 // therefore reads its whole tile (keys, values, scale bytes, scores) into registers, says so, waits until the tiles before it have been read, and writes.
 // Blocks draw their tiles in order: the tiles that one waits for were drawn before it, by blocks that are running and read without waiting for anything, so every
 // wait ends.  What bounds it: memory, read and written once (16 histories of 8192 tokens in 8 heads halved, 541 MB, 116 us, 4.7 TB/s: a copy's rate; a block to a
-// sequence and head, tile after tile, took 394); for short lists a chain of loads (list, page table, rows) behind a launch, 3.5 us.
+// sequence and head, tile after tile, took 394; 256 such histories, 2048 lists, have more tiles than there are words of state and go that way: 1819 us,
+// the same rate); for short lists a chain of loads (list, page table, rows) behind a launch, 3.5 us.
 #include "kv.h"
 
 namespace moe {
