@@ -46,6 +46,7 @@ def test_marks_of_the_built_kernels():
     src, kernel = next(iter(build.MARKS_BEFORE_COUNTS.items()))
     asm = os.path.join(build.OBJ, src.replace(".hip", "-hip-amdgcn-amd-amdhsa-gfx950.s"))
     if not os.path.exists(asm) or os.path.getmtime(asm) < os.path.getmtime(os.path.join(build.CSRC, src)):
+        os.makedirs(build.OBJ, exist_ok=True)
         build._compile(src, False)
     with open(asm) as f:
         text = f.read()
