@@ -771,7 +771,7 @@ template <typename T, bool FP8, int DP> hipError_t launch_by_rows(WeightArgs a, 
     //     255 bf16 160 / 166 (82 / 77), FP8 143 / 125 (83 / 76), fp32 528 / 488
     //   groups of 4, 8 heads: 40 bf16 90 / 96 (68 / 66), FP8 87 / 81 (67 / 66), fp32 386 / 373; 255 bf16 262 / 255 (106 / 79), FP8 221 / 174 (110 / 75), fp32 762 / 670
     //   groups of one, 8 heads: 10 bf16 37 / 41 (31 / 33), FP8 39 / 39 (32 / 35), fp32 117 / 116; 255 bf16 235 / 223 (74 / 46), FP8 192 / 144 (79 / 44), fp32 547 / 452
-    // (What two launches lose near the line, in bf16 above all, is a few us; what they save behind it grows with the decode rows, the more the fewer heads a group has.)
+    // (What two launches lose near the line, in bf16 above all, is up to 7 us; what they save behind it grows with the decode rows, the more the fewer heads a group has.)
     constexpr int kMostRows = 384;
     const int64_t rows = a.c.T, seqs = a.c.S, most = rows < seqs ? rows : rows - seqs + 1;
     if (rows * a.G <= kFewRows * seqs && most * a.G <= kMostRows) {
